@@ -15,6 +15,7 @@ LIB_PATH = os.path.join(HERE, "libjagg.so")
 
 F32, BF16 = 0, 1
 DGRAD, DGRAD_GELU, WGRAD = 0, 1, 2
+E4M3, E5M2 = 0, 1
 
 
 class _DitConfig(ctypes.Structure):
@@ -36,6 +37,15 @@ class _TensorDesc(ctypes.Structure):
                 ("rows", ctypes.c_int), ("cols", ctypes.c_int)]
 
 
+class _Mat8(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("ld", ctypes.c_size_t), ("rows", ctypes.c_int),
+                ("k", ctypes.c_int), ("fmt", ctypes.c_int)]
+
+
+class _Grad(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_size_t), ("dtype", ctypes.c_int)]
+
+
 _lib = None
 
 
@@ -48,7 +58,7 @@ def lib() -> ctypes.CDLL:
                                "(there is no fallback path)")
         L = ctypes.CDLL(LIB_PATH)
         vp, sz, i, f, d = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_float, ctypes.c_double
-        pcfg = ctypes.POINTER(_DitConfig)
+        pcfg, pm8, pg = ctypes.POINTER(_DitConfig), ctypes.POINTER(_Mat8), ctypes.POINTER(_Grad)
         L.jagg_last_error.restype = ctypes.c_char_p
         sig = {
             "dit_param_layout": [pcfg, ctypes.POINTER(sz), ctypes.POINTER(sz), ctypes.POINTER(_TensorDesc), sz],
@@ -73,6 +83,14 @@ def lib() -> ctypes.CDLL:
             "jagg_count_nonfinite": [vp, vp, sz, i, ctypes.POINTER(ctypes.c_ulonglong)],
             "jagg_window_quality": [vp, vp, vp, ctypes.POINTER(vp), i, ctypes.POINTER(vp), ctypes.POINTER(f), i, vp, vp,
                                     vp, ctypes.POINTER(d)],
+            "jagg_mat8_bytes": [i, i, ctypes.POINTER(sz), ctypes.POINTER(sz), ctypes.POINTER(sz)],
+            "jagg_quantize8": [vp, vp, sz, i, i, i, vp, vp, i, pm8, pm8],
+            "jagg_matmul8": [vp, pm8, pm8, vp, vp, sz, i, f],
+            "jagg_rmsnorm8": [vp, vp, sz, vp, sz, vp, i, i, i, f, vp, sz, pm8, vp],
+            "jagg_rmsnorm8_grad_bytes": [i, i, ctypes.POINTER(sz)],
+            "jagg_rmsnorm8_grad": [vp, vp, sz, vp, sz, vp, vp, vp, sz, i, i, i, vp, sz, vp, i, f],
+            "jagg_grad_norm": [vp, pg, i, i, vp],
+            "jagg_grad_clip": [vp, pg, pg, i, i, d, vp],
             "jagg_grpo_composites": [vp, ctypes.POINTER(_GrpoWindow), i, vp, vp, vp],
             "jagg_grpo_upstream": [vp, ctypes.POINTER(_GrpoWindow), i, ctypes.POINTER(vp), vp],
             "jagg_grpo_group_backward": [vp, vp, vp, i, ctypes.POINTER(_GrpoWindow), vp, f, vp],
@@ -189,6 +207,91 @@ def _torch():
     return torch
 
 
+# -------------------------------------------------- arguments of the operators
+def _refuse(msg: str):
+    raise JaggError(1, msg)
+
+
+def _dtype_of(t, name: str) -> int:
+    torch = _torch()
+    if t.dtype is torch.bfloat16:
+        return BF16
+    if t.dtype is torch.float32:
+        return F32
+    _refuse(f"{name} must be bf16 or fp32")
+
+
+def _vec(t, name: str, n: int, dtype, device):
+    """Pointer of a contiguous vector of n elements."""
+    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1) or t.device != device:
+        _refuse(f"{name} must be a contiguous vector of {n} elements of {dtype} on {device}")
+    return t.data_ptr()
+
+
+def _rows(t, name: str, rows: int, cols: int, dtype, device):
+    """(pointer, row stride) of a matrix whose rows are contiguous."""
+    if t.dtype is not dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.device != device:
+        _refuse(f"{name} must be {rows} x {cols} of {dtype} on {device}")
+    st = t.stride()
+    if (cols > 1 and st[1] != 1) or (rows > 1 and st[0] < cols):
+        _refuse(f"{name} must have contiguous rows that do not overlap")
+    return t.data_ptr(), st[0] if rows > 1 else cols
+
+
+class Mat8:
+    """An 8-bit matrix with one power-of-two scale per block of 128 columns
+    (jagg_mat8): ``q`` uint8 [rows][ld], ``scale`` uint8 [ceil(k/512)][rows][4].
+    Allocates both on the current CUDA device, or takes given tensors."""
+
+    def __init__(self, rows: int, k: int, fmt: int = E4M3, q=None, scale=None):
+        torch = _torch()
+        ld, nq, ns = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_size_t()
+        _check(lib().jagg_mat8_bytes(rows, k, ctypes.byref(ld), ctypes.byref(nq), ctypes.byref(ns)))
+        if fmt not in (E4M3, E5M2):
+            _refuse("unknown 8-bit format")
+        words = (k + 511) // 512
+        if q is None:
+            q = torch.empty(rows, ld.value, dtype=torch.uint8, device="cuda")
+        if scale is None:
+            scale = torch.empty(words, rows, 4, dtype=torch.uint8, device=q.device)
+        if q.element_size() != 1 or q.dim() != 2 or q.shape[0] != rows or q.shape[1] < ld.value or not q.is_contiguous():
+            _refuse(f"q must be contiguous bytes [{rows}][>= {ld.value}]")
+        if scale.element_size() != 1 or tuple(scale.shape) != (words, rows, 4) or not scale.is_contiguous():
+            _refuse(f"scale must be contiguous bytes [{words}][{rows}][4]")
+        if scale.device != q.device or not q.is_cuda:
+            _refuse("q and scale must be on one GPU")
+        self.rows, self.k, self.fmt = rows, k, fmt
+        self.q, self.scale = q.view(torch.uint8), scale.view(torch.uint8)
+        self.device = q.device
+        self._c = _Mat8(q.data_ptr(), scale.data_ptr(), q.shape[1], rows, k, fmt)
+
+
+class GradList:
+    """Gradient tensors (each contiguous, bf16 or fp32, of one GPU) as the norm and
+    clipping calls take them; a program that keeps its gradients keeps one."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        if not self.tensors:
+            _refuse("a gradient list needs a tensor")
+        self.device = self.tensors[0].device
+        self._c = (_Grad * len(self.tensors))()
+        for g, t in zip(self._c, self.tensors):
+            if not t.is_cuda or t.device != self.device or not t.is_contiguous():
+                _refuse("gradients must be contiguous tensors of one GPU")
+            g.data, g.n, g.dtype = t.data_ptr(), t.numel(), _dtype_of(t, "a gradient")
+        self.spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in self.tensors if t.numel())
+        if any(a[1] > b[0] for a, b in zip(self.spans, self.spans[1:])):
+            _refuse("gradients must not overlap")
+
+
+def _grads(g) -> GradList:
+    return g if isinstance(g, GradList) else GradList([g] if _torch().is_tensor(g) else g)
+
+
+_NORMS = {2: 0, 2.0: 0, float("inf"): 1}
+
+
 class Context:
     """One model configuration bound to a HIP stream, with a workspace tensor."""
 
@@ -198,10 +301,13 @@ class Context:
         self.stream = stream if stream is not None else torch.cuda.current_stream()
         h = ctypes.c_void_p()
         c = cfg.c()
-        _check(lib().jagg_ctx_create(ctypes.byref(c), ctypes.c_void_p(self.stream.cuda_stream), ctypes.byref(h)))
+        self.device = self.stream.device
+        with torch.cuda.device(self.device):
+            _check(lib().jagg_ctx_create(ctypes.byref(c), ctypes.c_void_p(self.stream.cuda_stream), ctypes.byref(h)))
         self._h = h
         self._ws = None
-        self._ws_batch = 0
+        self._ws_batch = self._ws_bytes = 0
+        self._in_graph, self._ws_of_graphs = False, []
         self.layout, self.n_params = param_layout(cfg)
 
     def __del__(self):
@@ -232,14 +338,26 @@ class Context:
 
     def ensure_workspace(self, batch: int):
         if self._ws is not None and self._ws_batch >= batch:
+            self._ensure_bytes(0)
             return
+        self._ensure_bytes(self.workspace_bytes(batch))
+        self._ws_batch = batch
+
+    def _ensure_bytes(self, nb: int):
+        """A bound workspace of at least nb bytes (it only grows)."""
         torch = _torch()
-        nb = self.workspace_bytes(batch)
-        self._ws = torch.empty(nb + 256, dtype=torch.uint8, device="cuda")
-        base = self._ws.data_ptr()
+        if torch.cuda.is_current_stream_capturing():
+            self._in_graph = True
+        if self._ws is not None and self._ws_bytes >= nb:
+            return
+        if self._in_graph:  # a captured graph may hold the workspace's address: it stays
+            self._ws_of_graphs.append(self._ws)
+        with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
+            ws = torch.empty(nb + 256, dtype=torch.uint8, device=self.device)
+        base = ws.data_ptr()
         off = (-base) % 256
         _check(lib().jagg_ctx_set_workspace(self._h, ctypes.c_void_p(base + off), nb))
-        self._ws_batch = batch
+        self._ws, self._ws_bytes = ws, nb
 
     def new_saved(self, batch: int):
         torch = _torch()
@@ -394,6 +512,111 @@ class Context:
                                       None if pre is None else pre.data_ptr(), rows, n_out, n_in, result.data_ptr(),
                                       rdt, float(beta)))
         return result
+
+    # ------------------------------------------- 8-bit linear layers, clipping
+    def quantize8(self, x, out: Mat8 = None, out_t: Mat8 = None, tile: bool = False, row_mul=None, col_mul=None):
+        """8-bit form of y = x * row_mul[:, None] * col_mul: ``out`` its rows (blocks
+        of 128 along a row), ``out_t`` its transpose (blocks along a column), either
+        or both; ``tile``: one scale per 128 x 128, the same in both."""
+        if x.dim() != 2:
+            _refuse("x must be a matrix")
+        rows, cols = x.shape
+        dt = _dtype_of(x, "x")
+        p, ld = _rows(x, "x", rows, cols, x.dtype, self.device)
+        for m in (out, out_t):
+            if m is not None and m.device != self.device:
+                _refuse("out and out_t must be on the context's device")
+        rm = None if row_mul is None else _vec(row_mul, "row_mul", rows, _torch().float32, self.device)
+        cm = None if col_mul is None else _vec(col_mul, "col_mul", cols, x.dtype, self.device)
+        _check(lib().jagg_quantize8(self._h, p, ld, rows, cols, dt, rm, cm, 1 if tile else 0,
+                                    None if out is None else out._c, None if out_t is None else out_t._c))
+        return out, out_t
+
+    def matmul8(self, a: Mat8, b: Mat8, out, bias=None, beta: float = 0.0):
+        """out = beta * out + a b^T + bias (out: [a.rows][b.rows], bf16 or fp32)."""
+        dt = _dtype_of(out, "out")
+        p, ld = _rows(out, "out", a.rows, b.rows, out.dtype, self.device)
+        if a.device != self.device or b.device != self.device:
+            _refuse("the operands must be on the context's device")
+        bp = None if bias is None else _vec(bias, "bias", b.rows, out.dtype, self.device)
+        _check(lib().jagg_matmul8(self._h, a._c, b._c, bp, p, ld, dt, beta))
+        return out
+
+    def rmsnorm8(self, x, gain, y: Mat8, residual=None, h=None, rstd=None, eps: float = 1e-6):
+        """h = x + residual, y = h / sqrt(mean(h^2) + eps) * gain in 8 bits (E4M3);
+        ``h`` and ``rstd`` are written if given (the backward reads both)."""
+        if x.dim() != 2:
+            _refuse("x must be a matrix")
+        rows, cols = x.shape
+        dt, dev = _dtype_of(x, "x"), self.device
+        p, ld = _rows(x, "x", rows, cols, x.dtype, dev)
+        rp, rl = (None, 0) if residual is None else _rows(residual, "residual", rows, cols, x.dtype, dev)
+        hp, hl = (None, 0) if h is None else _rows(h, "h", rows, cols, x.dtype, dev)
+        if y.device != dev:
+            _refuse("y must be on the context's device")
+        _check(lib().jagg_rmsnorm8(self._h, p, ld, rp, rl, _vec(gain, "gain", cols, x.dtype, dev), rows, cols, dt, eps,
+                                   hp, hl, y._c, None if rstd is None else _vec(rstd, "rstd", rows, _torch().float32, dev)))
+        return y
+
+    def rmsnorm8_grad(self, dy, h, rstd, gain, dx, dgain, dh=None, beta: float = 0.0):
+        """Backward of rmsnorm8: dx (of x and of the residual; dh, the gradient of h
+        from elsewhere, is added) and dgain = beta * dgain + its gradient."""
+        if h.dim() != 2:
+            _refuse("h must be a matrix")
+        rows, cols = h.shape
+        dt, dev = _dtype_of(h, "h"), self.device
+        yp, yl = _rows(dy, "dy", rows, cols, h.dtype, dev)
+        hp, hl = _rows(h, "h", rows, cols, h.dtype, dev)
+        gp, gl = (None, 0) if dh is None else _rows(dh, "dh", rows, cols, h.dtype, dev)
+        xp, xl = _rows(dx, "dx", rows, cols, h.dtype, dev)
+        nb = ctypes.c_size_t()
+        _check(lib().jagg_rmsnorm8_grad_bytes(rows, cols, ctypes.byref(nb)))
+        self._ensure_bytes(nb.value)
+        _check(lib().jagg_rmsnorm8_grad(self._h, yp, yl, hp, hl, _vec(rstd, "rstd", rows, _torch().float32, dev),
+                                        _vec(gain, "gain", cols, h.dtype, dev), gp, gl, rows, cols, dt, xp, xl,
+                                        _vec(dgain, "dgain", cols, dgain.dtype, dev), _dtype_of(dgain, "dgain"), beta))
+        return dx, dgain
+
+    def grad_norm(self, grads, out, ord=2):
+        """Global norm (2 or inf) of a tensor, a list of tensors or a GradList into
+        ``out`` (device fp64 tensor of one element)."""
+        g = _grads(grads)
+        if g.device != self.device or ord not in _NORMS:
+            _refuse("the gradients must be on the context's device, ord 2 or inf")
+        p = _vec(out, "out", 1, _torch().float64, self.device)
+        self.ensure_workspace(1)
+        _check(lib().jagg_grad_norm(self._h, g._c, len(g.tensors), _NORMS[ord], p))
+        return out
+
+    def clip_grads(self, grads, max_norm: float, out, dst=None, ord=2):
+        """Scales the gradients (in place, or into ``dst``, tensors of the same sizes)
+        so that their global norm is at most max_norm; out (device fp64 tensor of
+        two elements) receives the norm and the factor.  A norm that is not finite
+        leaves the values as they are."""
+        g = _grads(grads)
+        d = None if dst is None else _grads(dst)
+        if g.device != self.device or ord not in _NORMS:
+            _refuse("the gradients must be on the context's device, ord 2 or inf")
+        if d is not None:
+            if d.device != self.device or len(d.tensors) != len(g.tensors):
+                _refuse("dst must have one tensor on the context's device for each gradient")
+            # lists that lie apart as a whole need no closer look
+            apart = not g.spans or not d.spans or d.spans[-1][1] <= g.spans[0][0] or g.spans[-1][1] <= d.spans[0][0]
+            if not (apart or d is g):
+                self._check_dst(g, d)
+        p = _vec(out, "out", 2, _torch().float64, self.device)
+        self.ensure_workspace(1)
+        _check(lib().jagg_grad_clip(self._h, g._c, None if d is None else d._c, len(g.tensors), _NORMS[ord],
+                                    float(max_norm), p))
+        return out
+
+    @staticmethod
+    def _check_dst(g: GradList, d: GradList):
+        own = {a.data_ptr() for a, b in zip(g.tensors, d.tensors)
+               if a.data_ptr() == b.data_ptr() and a.dtype is b.dtype and a.numel() == b.numel()}
+        both = sorted(g.spans + [s for s in d.spans if s[0] not in own])
+        if any(a[1] > b[0] for a, b in zip(both, both[1:])):
+            _refuse("dst must not overlap the gradients, but for a tensor's own")
 
     def trajectory_backward(self, theta, W: int, batch: int, saved_pairs, saved_steps, s_list, t, use_jagg, dtheta,
                             beta: float = 0.0):

@@ -14,6 +14,7 @@
 #include "attention.h"
 #include "gemm.h"
 #include "ops.h"
+#include "ops8.h"
 #include "prof.h"
 
 namespace jg {
@@ -344,6 +345,7 @@ struct jagg_ctx {
   // first use (default priority), with its fork and join events
   hipStream_t side = nullptr;
   hipEvent_t fork = nullptr, join = nullptr, mark = nullptr;
+  int device = -1;  // of the stream (-1: no device when the context was made)
 };
 
 namespace jg {
@@ -1019,6 +1021,9 @@ jagg_status jagg_ctx_create(const dit_config* cfg, void* hip_stream, jagg_ctx** 
   if (!c) return fail(JAGG_ENOMEM, "jagg_ctx_create: out of host memory");
   if (jg::build_model(*cfg, c->m)) { delete c; return JAGG_EINVAL; }
   c->stream = (hipStream_t)hip_stream;
+  hipDevice_t dev = -1;
+  if ((hip_stream ? hipStreamGetDevice(c->stream, &dev) : hipGetDevice(&dev)) == hipSuccess) c->device = dev;
+  else (void)hipGetLastError();
   *out = c;
   return JAGG_OK;
 }
@@ -1263,6 +1268,226 @@ jagg_status jagg_linear_grad(jagg_ctx* ctx, int kind, const void* dY, const void
     }
   }
   return to_status(jg::gemm(g, ctx->stream));
+}
+
+}  // extern "C"
+
+// ------------------------------------- 8-bit linear layers, gradient clipping
+namespace {
+
+// The context's device is the current one while a call launches.
+struct OnDevice {
+  int was = -1;
+  explicit OnDevice(const jagg_ctx* ctx) {
+    int now = -1;
+    if (ctx->device < 0 || hipGetDevice(&now) != hipSuccess || now == ctx->device) return;
+    if (hipSetDevice(ctx->device) == hipSuccess) was = now;
+  }
+  ~OnDevice() {
+    if (was >= 0) (void)hipSetDevice(was);
+  }
+};
+
+bool is_dtype(int d) { return d == JAGG_F32 || d == JAGG_BF16; }
+bool misaligned(const void* p, size_t to) { return (uintptr_t)p % to != 0; }
+
+constexpr size_t MAT8_MAX_LD = 1u << 22;
+
+// What is wrong with an 8-bit matrix, or nullptr.
+const char* mat8_fault(const jagg_mat8* m) {
+  if (!m->q || !m->scale) return "null buffer";
+  if (m->rows < 1 || m->k < 1) return "rows and k must be >= 1";
+  if (m->fmt != JAGG_E4M3 && m->fmt != JAGG_E5M2) return "unknown format";
+  if (m->ld % 128 || m->ld < ((size_t)m->k + 127) / 128 * 128) return "ld must be a multiple of 128 and >= k";
+  if (m->ld > MAT8_MAX_LD) return "ld must be <= 4194304";
+  if (misaligned(m->q, 16) || misaligned(m->scale, 4)) return "q must be 16-byte and scale 4-byte aligned";
+  return nullptr;
+}
+jg::Mat8 to_mat8(const jagg_mat8* m) {
+  jg::Mat8 r;
+  r.q = (uint8_t*)m->q;
+  r.sc = (uint32_t*)m->scale;
+  r.ld = m->ld;
+  r.rows = m->rows;
+  r.k = m->k;
+  r.fmt = m->fmt;
+  return r;
+}
+
+jagg_status grad_list_check(const jagg_ctx* ctx, const jagg_grad* g, const jagg_grad* dst, int count, int ord,
+                            const double* out, const char* f) {
+  if (!ctx || !g || !out) return fail(JAGG_EINVAL, std::string(f) + ": null argument");
+  if (count < 1) return fail(JAGG_EINVAL, std::string(f) + ": count must be >= 1");
+  if (ord != JAGG_NORM_L2 && ord != JAGG_NORM_MAX) return fail(JAGG_EINVAL, std::string(f) + ": unknown norm");
+  if (misaligned(out, 8)) return fail(JAGG_EINVAL, std::string(f) + ": the result must be 8-byte aligned");
+  for (int i = 0; i < count; ++i)
+    for (const jagg_grad* p : {g + i, dst ? dst + i : g + i}) {
+      if (!is_dtype(p->dtype)) return fail(JAGG_EINVAL, std::string(f) + ": unknown dtype");
+      if (p->n != g[i].n) return fail(JAGG_EINVAL, std::string(f) + ": a copy has another size than its tensor");
+      if (p->n == 0) continue;
+      if (p != g + i && p->data == g[i].data && p->dtype != g[i].dtype)
+        return fail(JAGG_EINVAL, std::string(f) + ": a copy in place has its tensor's dtype");
+      if (!p->data) return fail(JAGG_EINVAL, std::string(f) + ": null tensor");
+      if (misaligned(p->data, jg::dsize(p->dtype)))
+        return fail(JAGG_EINVAL, std::string(f) + ": a tensor is not aligned to its elements");
+    }
+  return JAGG_OK;
+}
+struct GradLists { const jagg_grad *src, *dst; };
+jg::GradSeg grad_at(const void* list, int i) {
+  const GradLists* l = (const GradLists*)list;
+  return {l->src[i].data, l->dst ? l->dst[i].data : nullptr, l->src[i].n, l->src[i].dtype,
+          l->dst ? l->dst[i].dtype : l->src[i].dtype};
+}
+
+}  // namespace
+
+extern "C" {
+
+jagg_status jagg_mat8_bytes(int rows, int k, size_t* ld, size_t* q_bytes, size_t* scale_bytes) {
+  if (!ld || !q_bytes || !scale_bytes) return fail(JAGG_EINVAL, "jagg_mat8_bytes: null argument");
+  if (rows < 1 || k < 1) return fail(JAGG_EINVAL, "jagg_mat8_bytes: rows and k must be >= 1");
+  *ld = ((size_t)k + 127) / 128 * 128;
+  *q_bytes = *ld * rows;
+  *scale_bytes = ((size_t)k + 511) / 512 * rows * 4;
+  return JAGG_OK;
+}
+
+jagg_status jagg_quantize8(jagg_ctx* ctx, const void* x, size_t ldx, int rows, int cols, int dtype,
+                           const float* row_mul, const void* col_mul, int tile, const jagg_mat8* out,
+                           const jagg_mat8* out_t) {
+  const char* f = "jagg_quantize8: ";
+  if (!ctx || !x || (!out && !out_t)) return fail(JAGG_EINVAL, std::string(f) + "null argument");
+  if (rows < 1 || cols < 1) return fail(JAGG_EINVAL, std::string(f) + "sizes must be >= 1");
+  if (!is_dtype(dtype)) return fail(JAGG_EINVAL, std::string(f) + "unknown dtype");
+  if (tile != 0 && tile != 1) return fail(JAGG_EINVAL, std::string(f) + "tile must be 0 or 1");
+  if (ldx < (size_t)cols) return fail(JAGG_EINVAL, std::string(f) + "ldx must be >= cols");
+  if (misaligned(x, jg::dsize(dtype)) || misaligned(col_mul, jg::dsize(dtype)) || misaligned(row_mul, 4))
+    return fail(JAGG_EINVAL, std::string(f) + "a buffer is not aligned to its elements");
+  for (const jagg_mat8* m : {out, out_t})
+    if (m)
+      if (const char* e = mat8_fault(m)) return fail(JAGG_EINVAL, std::string(f) + e);
+  if (out && (out->rows != rows || out->k != cols)) return fail(JAGG_EINVAL, std::string(f) + "out must be rows x cols");
+  if (out_t && (out_t->rows != cols || out_t->k != rows))
+    return fail(JAGG_EINVAL, std::string(f) + "out_t must be cols x rows");
+  if (out && out_t && out->fmt != out_t->fmt) return fail(JAGG_EINVAL, std::string(f) + "out and out_t differ in format");
+  if ((((size_t)rows + 127) / 128) * (((size_t)cols + 127) / 128) > 0x7fffffffu)
+    return fail(JAGG_EUNSUPPORTED, std::string(f) + "too many 128 x 128 tiles");
+  jg::Quant8Args a{};
+  a.x = x; a.ldx = ldx; a.rows = rows; a.cols = cols; a.dt = dtype;
+  a.row_mul = row_mul; a.col_mul = col_mul; a.tile = tile;
+  if (out) a.out = to_mat8(out);
+  if (out_t) a.out_t = to_mat8(out_t);
+  a.fmt = out ? out->fmt : out_t->fmt;
+  OnDevice dev(ctx);
+  return to_status(jg::quant8(a, ctx->stream));
+}
+
+jagg_status jagg_matmul8(jagg_ctx* ctx, const jagg_mat8* a, const jagg_mat8* b, const void* bias, void* out, size_t ldo,
+                         int out_dtype, float beta) {
+  const char* f = "jagg_matmul8: ";
+  if (!ctx || !a || !b || !out) return fail(JAGG_EINVAL, std::string(f) + "null argument");
+  for (const jagg_mat8* m : {a, b})
+    if (const char* e = mat8_fault(m)) return fail(JAGG_EINVAL, std::string(f) + e);
+  if (a->k != b->k) return fail(JAGG_EINVAL, std::string(f) + "the operands differ in k");
+  if (b->fmt != JAGG_E4M3) return fail(JAGG_EUNSUPPORTED, std::string(f) + "the right operand must be E4M3");
+  if (!is_dtype(out_dtype)) return fail(JAGG_EINVAL, std::string(f) + "unknown result dtype");
+  if (beta != 0.f && beta != 1.f) return fail(JAGG_EINVAL, std::string(f) + "beta must be 0 or 1");
+  if (ldo < (size_t)b->rows) return fail(JAGG_EINVAL, std::string(f) + "ldo must be >= the right operand's rows");
+  if (misaligned(out, jg::dsize(out_dtype)) || misaligned(bias, jg::dsize(out_dtype)))
+    return fail(JAGG_EINVAL, std::string(f) + "a buffer is not aligned to its elements");
+  if ((((size_t)a->rows + 63) / 64) * (((size_t)b->rows + 63) / 64) > 0x7fffffffu)
+    return fail(JAGG_EUNSUPPORTED, std::string(f) + "too many tiles");
+  jg::Matmul8Args g{};
+  g.a = to_mat8(a); g.b = to_mat8(b);
+  g.bias = bias;
+  g.out = out; g.ldo = ldo; g.out_dt = out_dtype;
+  g.beta = beta;
+  OnDevice dev(ctx);
+  return to_status(jg::matmul8(g, ctx->stream));
+}
+
+jagg_status jagg_rmsnorm8(jagg_ctx* ctx, const void* x, size_t ldx, const void* residual, size_t ldr, const void* gain,
+                          int rows, int cols, int dtype, float eps, void* h, size_t ldh, const jagg_mat8* y,
+                          float* rstd) {
+  const char* f = "jagg_rmsnorm8: ";
+  if (!ctx || !x || !gain || !y) return fail(JAGG_EINVAL, std::string(f) + "null argument");
+  if (rows < 1 || cols < 1) return fail(JAGG_EINVAL, std::string(f) + "sizes must be >= 1");
+  if (cols > jg::NORM8_MAX_COLS) return fail(JAGG_EUNSUPPORTED, std::string(f) + "cols must be <= 32768");
+  if (!is_dtype(dtype)) return fail(JAGG_EINVAL, std::string(f) + "unknown dtype");
+  if (!(eps >= 0.f) || std::isinf(eps)) return fail(JAGG_EINVAL, std::string(f) + "eps must be >= 0 and finite");
+  if (ldx < (size_t)cols || (residual && ldr < (size_t)cols) || (h && ldh < (size_t)cols))
+    return fail(JAGG_EINVAL, std::string(f) + "row strides must be >= cols");
+  const size_t es = jg::dsize(dtype);
+  if (misaligned(x, es) || misaligned(residual, es) || misaligned(gain, es) || misaligned(h, es) || misaligned(rstd, 4))
+    return fail(JAGG_EINVAL, std::string(f) + "a buffer is not aligned to its elements");
+  if (const char* e = mat8_fault(y)) return fail(JAGG_EINVAL, std::string(f) + e);
+  if (y->rows != rows || y->k != cols) return fail(JAGG_EINVAL, std::string(f) + "y must be rows x cols");
+  if (y->fmt != JAGG_E4M3) return fail(JAGG_EUNSUPPORTED, std::string(f) + "y must be E4M3");
+  jg::Norm8Args a{};
+  a.x = x; a.ldx = ldx; a.r = residual; a.ldr = ldr; a.gain = gain;
+  a.rows = rows; a.cols = cols; a.dt = dtype; a.eps = eps;
+  a.h = h; a.ldh = ldh; a.y = to_mat8(y); a.rstd = rstd;
+  OnDevice dev(ctx);
+  return to_status(jg::rmsnorm8(a, ctx->stream));
+}
+
+jagg_status jagg_rmsnorm8_grad_bytes(int rows, int cols, size_t* bytes) {
+  if (!bytes) return fail(JAGG_EINVAL, "jagg_rmsnorm8_grad_bytes: null argument");
+  if (rows < 1 || cols < 1) return fail(JAGG_EINVAL, "jagg_rmsnorm8_grad_bytes: sizes must be >= 1");
+  *bytes = jg::rmsnorm8_grad_bytes(rows, cols);
+  return JAGG_OK;
+}
+
+jagg_status jagg_rmsnorm8_grad(jagg_ctx* ctx, const void* dy, size_t lddy, const void* h, size_t ldh, const float* rstd,
+                               const void* gain, const void* dh, size_t lddh, int rows, int cols, int dtype, void* dx,
+                               size_t lddx, void* dgain, int dgain_dtype, float beta) {
+  const char* f = "jagg_rmsnorm8_grad: ";
+  if (!ctx || !dy || !h || !rstd || !gain || !dx || !dgain) return fail(JAGG_EINVAL, std::string(f) + "null argument");
+  if (rows < 1 || cols < 1) return fail(JAGG_EINVAL, std::string(f) + "sizes must be >= 1");
+  if (cols > jg::NORM8_MAX_COLS) return fail(JAGG_EUNSUPPORTED, std::string(f) + "cols must be <= 32768");
+  if (!is_dtype(dtype) || !is_dtype(dgain_dtype)) return fail(JAGG_EINVAL, std::string(f) + "unknown dtype");
+  if (beta != 0.f && beta != 1.f) return fail(JAGG_EINVAL, std::string(f) + "beta must be 0 or 1");
+  if (lddy < (size_t)cols || ldh < (size_t)cols || (dh && lddh < (size_t)cols) || lddx < (size_t)cols)
+    return fail(JAGG_EINVAL, std::string(f) + "row strides must be >= cols");
+  const size_t es = jg::dsize(dtype);
+  if (misaligned(dy, es) || misaligned(h, es) || misaligned(gain, es) || misaligned(dh, es) || misaligned(dx, es) ||
+      misaligned(rstd, 4) || misaligned(dgain, jg::dsize(dgain_dtype)))
+    return fail(JAGG_EINVAL, std::string(f) + "a buffer is not aligned to its elements");
+  const size_t need = jg::rmsnorm8_grad_bytes(rows, cols);
+  if (!ctx->ws || ctx->ws_bytes < need)
+    return fail(JAGG_EINVAL, std::string(f) + "workspace not bound or smaller than jagg_rmsnorm8_grad_bytes = " +
+                                 std::to_string(need));
+  jg::Norm8Grad a{};
+  a.dy = dy; a.lddy = lddy; a.h = h; a.ldh = ldh; a.rstd = rstd; a.gain = gain; a.dh = dh; a.lddh = lddh;
+  a.rows = rows; a.cols = cols; a.dt = dtype;
+  a.dx = dx; a.lddx = lddx; a.dgain = dgain; a.dgain_dt = dgain_dtype; a.beta = beta;
+  a.part = (float*)ctx->ws;
+  OnDevice dev(ctx);
+  return to_status(jg::rmsnorm8_grad(a, ctx->stream));
+}
+
+jagg_status jagg_grad_norm(jagg_ctx* ctx, const jagg_grad* g, int count, int ord, double* norm) {
+  const char* f = "jagg_grad_norm";
+  if (jagg_status st = grad_list_check(ctx, g, nullptr, count, ord, norm, f)) return st;
+  jg::Ws W0;
+  if (jagg_status st = need_head_ws(ctx, W0, f)) return st;
+  const GradLists l{g, nullptr};
+  OnDevice dev(ctx);
+  return to_status(jg::grad_norm(grad_at, &l, count, ord == JAGG_NORM_MAX, W0.spart, norm, ctx->stream));
+}
+
+jagg_status jagg_grad_clip(jagg_ctx* ctx, const jagg_grad* g, const jagg_grad* dst, int count, int ord, double max_norm,
+                           double* out) {
+  const char* f = "jagg_grad_clip";
+  if (jagg_status st = grad_list_check(ctx, g, dst, count, ord, out, f)) return st;
+  if (!(max_norm >= 0.0) || std::isinf(max_norm))
+    return fail(JAGG_EINVAL, std::string(f) + ": max_norm must be >= 0 and finite");
+  jg::Ws W0;
+  if (jagg_status st = need_head_ws(ctx, W0, f)) return st;
+  const GradLists l{g, dst ? dst : g};
+  OnDevice dev(ctx);
+  return to_status(jg::grad_clip(grad_at, &l, count, ord == JAGG_NORM_MAX, max_norm, W0.spart, out, ctx->stream));
 }
 
 jagg_status jagg_group_backward(jagg_ctx* ctx, const void* theta, const void* saved_pair, int batch,
