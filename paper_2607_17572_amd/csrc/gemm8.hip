@@ -16,12 +16,16 @@
 // fp32 results: the values as bf16 (every 8-bit value with its scale is one:
 // v_cvt_scalef32_pk_bf16_fp8) through v_mfma_f32_32x32x16_bf16, whose sums are fp32,
 // at half the rate.
+#include <type_traits>
+
 #include "q8.h"
+#include "tile.h"
 
 namespace jg {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -47,63 +51,370 @@ __device__ __forceinline__ bf16x8 widen8(int w0, int w1, float s) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// One wave per 32 x 32 tile of C, operands straight from memory.
-template <int FA, typename T>
-__global__ __launch_bounds__(256) void matmul8_k(Matmul8Args g) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int tiles_n = (g.b.rows + 63) / 64;
-  const int m0 = (int)(blockIdx.x / tiles_n) * 64 + (wave >> 1) * 32, n0 = (int)(blockIdx.x % tiles_n) * 64 + (wave & 1) * 32;
-  const int l = lane & 31, h = lane >> 5;
-  const int ra = min(m0 + l, g.a.rows - 1), rb = min(n0 + l, g.b.rows - 1);
-  const uint8_t* pa = g.a.q + (size_t)ra * g.a.ld + 32 * h;
-  const uint8_t* pb = g.b.q + (size_t)rb * g.b.ld + 32 * h;
-  f32x16 acc;
-  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-  const int nk = (g.a.k + 127) / 128;
-  for (int b = 0; b < nk; ++b) {
-    const int sa = (int)((g.a.sc[(size_t)(b >> 2) * g.a.rows + ra] >> (8 * (b & 3))) & 255u);
-    const int sb = (int)((g.b.sc[(size_t)(b >> 2) * g.b.rows + rb] >> (8 * (b & 3))) & 255u);
+// --------------------------------------------------------------- tiled kernel
+// BM x BN tiles, KG groups of WM x WN waves that split the k tiles and add their sums
+// through LDS.  k tiles of 64 bytes pass through four LDS stages, loaded three ahead
+// straight from memory (the layout, swizzle and barriers of the bf16 direct-to-LDS
+// kernel: 64 bytes are 32 of its k and 64 here, and an instruction takes twice the
+// bytes in twice the time, so its balance of loads, LDS reads and matrix
+// instructions carries over).  A fragment is 32 rows x 64 bytes: a lane takes chunks
+// h and h + 2 of its row (h = lane / 32), the same on both sides, so the order of k
+// inside the instruction differs from memory's and the sum does not.
+//
+// The instruction's left operand is B, so that a lane holds neighbouring columns of
+// one row of C.  A's fragments are read half a tile ahead: step 0 multiplies the
+// first half of A's fragments while the second half is read, step 1 the second half
+// while the next tile's B and first half are read.
+template <int ROWS, int NW, int WR>
+struct Op8 {
+  static constexpr int NL = ROWS / 16 / NW;  // direct loads of 1 KB per wave and k tile
+  static_assert(NL * 16 * NW == ROWS, "every wave loads the same");
+  int voff[NL];
+  int fo;  // chunk h of this lane's row of fragment 0; chunk h + 2 lies at fo ^ 32
+  __device__ inline void init(int ld, int wrow0) {
+    const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) % NW;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const i32x4 a0 = *(const i32x4*)(pa + b * 128 + t * 64), a1 = *(const i32x4*)(pa + b * 128 + t * 64 + 16);
-      const i32x4 b0 = *(const i32x4*)(pb + b * 128 + t * 64), b1 = *(const i32x4*)(pb + b * 128 + t * 64 + 16);
-      const i32x8 va = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
-      const i32x8 vb = __builtin_shufflevector(b0, b1, 0, 1, 2, 3, 4, 5, 6, 7);
-      if constexpr (sizeof(T) == 2) {
-        acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(va, vb, acc, FA, 0, 0, sa, 0, sb);
-      } else {
-        // k in any order, the same on both sides
-#pragma unroll
-        for (int w = 0; w < 8; w += 2)
-          acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8<FA>(va[w], va[w + 1], scale_of(sa)),
-                                                        widen8<E4M3>(vb[w], vb[w + 1], scale_of(sb)), acc, 0, 0, 0);
-      }
+    for (int t = 0; t < NL; ++t) {
+      const int row = 16 * (wave * NL + t) + lane / 4;
+      voff[t] = row * ld + 16 * ((lane % 4) ^ swz_n(row));
     }
+    const int r = lane & 31;
+    fo = (wrow0 + r) * 64 + ((lane >> 5) ^ swz_n(r)) * 16;
   }
-  const int n = n0 + l;
-  if (n >= g.b.rows) return;
-  const float bias = g.bias ? ldf((const T*)g.bias, n) : 0.f;
+  __device__ inline void load(__amdgpu_buffer_rsrc_t R, char* S, int k0) const {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % NW;
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const int m = m0 + 8 * (e / 4) + 4 * h + e % 4;
-    if (m >= g.a.rows) continue;
-    float v = acc[e] + bias;
-    T* c = (T*)g.out + (size_t)m * g.ldo;
-    if (g.beta != 0.f) v += ldf(c, n);
-    stf(c, n, v);
+    for (int t = 0; t < NL; ++t)
+      load_lds16(R, S + (wave * NL + t) * 1024, voff[t] + k0);
+  }
+  __device__ inline i32x8 frag(const char* S, int i) const {
+    const i32x4 a = *(const i32x4*)(S + fo + i * 2048), b = *(const i32x4*)(S + (fo ^ 32) + i * 2048);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+};
+
+// bias, old C and the store of eight (bf16) or four (fp32) columns of a row
+template <typename T, int NC>
+__device__ __forceinline__ void store_c(const Matmul8Args& g, int row, int col, float* v) {
+  T* c = (T*)g.out + (size_t)row * g.ldo + col;
+  const T* b = (const T*)g.bias + col;
+  if (col + NC <= g.b.rows) {
+    if constexpr (NC == 8) {
+      float o[8];
+      if (g.bias) {
+        load8(b, o);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += o[e];
+      }
+      if (g.beta != 0.f) {
+        load8(c, o);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += o[e];
+      }
+      store8(c, v);
+    } else {
+      u32x4a o;
+      if (g.bias) {
+        o = *(const u32x4a*)b;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += __uint_as_float(o[e]);
+      }
+      if (g.beta != 0.f) {
+        o = *(const u32x4a*)c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += __uint_as_float(o[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(v[e]);
+      *(u32x4a*)c = o;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < NC; ++e)
+      if (col + e < g.b.rows) {
+        float x = v[e];
+        if (g.bias) x += ldf(b, e);
+        if (g.beta != 0.f) x += ldf(c, e);
+        stf(c, e, x);
+      }
   }
 }
 
-template <int FA>
+template <int FA, typename T, int BM, int BN, int WM, int WN, int KG>
+__global__ __launch_bounds__(64 * WM * WN * KG) void matmul8_tile_k(Matmul8Args g) {
+  constexpr bool EXACT = sizeof(T) == 4;
+  constexpr int BK = 64, NW = WM * WN, FM = BM / (32 * WM), FN = BN / (32 * WN), HM = FM / 2;
+  static_assert(FM % 2 == 0, "A's fragments go in two halves");
+  constexpr int STG = (BM + BN) * BK, SB = BM * BK;
+  // one variable per stage: accesses name their stage statically (see wait_vm_lds)
+  __shared__ __attribute__((aligned(1024))) char st0[KG * STG];
+  __shared__ __attribute__((aligned(1024))) char st1[KG * STG];
+  __shared__ __attribute__((aligned(1024))) char st2[KG * STG];
+  __shared__ __attribute__((aligned(1024))) char st3[KG * STG];
+
+  const int M = g.a.rows, N = g.b.rows;
+  const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
+  int tm, tn;
+  tile_coords(xcd_remap(blockIdx.x, tiles_m * tiles_n), tiles_m, tiles_n, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN;
+  const int grp = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / NW;
+  const int lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
+  const int wave = (threadIdx.x >> 6) % NW, wm = wave / WN, wn = wave % WN;
+
+  typedef Op8<BM, NW, BM / WM> OpA;
+  typedef Op8<BN, NW, BN / WN> OpB;
+  OpA oa;
+  OpB ob;
+  oa.init((int)g.a.ld, wm * (BM / WM));
+  ob.init((int)g.b.ld, wn * (BN / WN));
+  // the tile's rows: offsets stay below 2^31 (ld <= 2^22), rows past the end and the
+  // prefetch behind the last row read zeros
+  const int kp = (g.a.k + 127) / 128 * 128;
+  const __amdgpu_buffer_rsrc_t RA = make_rsrc(g.a.q + (size_t)m0 * g.a.ld, (min(BM, M - m0) - 1) * (long)g.a.ld + kp);
+  const __amdgpu_buffer_rsrc_t RB = make_rsrc(g.b.q + (size_t)n0 * g.b.ld, (min(BN, N - n0) - 1) * (long)g.b.ld + kp);
+
+  // exponent words of this lane's row of each fragment (four blocks = eight k tiles)
+  uint32_t pa[FM], pb[FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i) pa[i] = min(m0 + wm * (BM / WM) + 32 * i + l, M - 1);
+#pragma unroll
+  for (int j = 0; j < FN; ++j) pb[j] = min(n0 + wn * (BN / WN) + 32 * j + l, N - 1);
+
+  f32x16 acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  auto stage = [&](auto ic) -> char* {
+    constexpr int c = decltype(ic)::value & 3;
+    if constexpr (c == 0) return st0 + grp * STG;
+    else if constexpr (c == 1) return st1 + grp * STG;
+    else if constexpr (c == 2) return st2 + grp * STG;
+    else return st3 + grp * STG;
+  };
+  // the group's k tiles: kt0 .. kt0 + nk - 1, kt0 a multiple of 8 (whole exponent words)
+  const int nkt = kp / BK, nkg = KG == 1 ? nkt : ((nkt + KG - 1) / KG + 7) / 8 * 8;
+  const int kt0 = grp * nkg, nk = KG == 1 ? nkt : max(0, min(nkg, nkt - kt0));
+  uint32_t wa[FM], wb[FN], na[FM], nb[FN];
+  auto words = [&](int t) {  // of k tile t (a multiple of 8); the last ones again behind the end
+    const size_t w = min(t, nkt - 1) / 8;
+    const uint32_t *sa = g.a.sc + w * M, *sb = g.b.sc + w * N;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) na[i] = sa[pa[i]];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) nb[j] = sb[pb[j]];
+  };
+
+  i32x8 fa[FM], fb[2][FN];
+  bf16x8 xb[EXACT ? FN : 1][4];
+  auto mfma_half = [&](int half, int buf) {
+    if constexpr (!EXACT) {
+#pragma unroll
+      for (int i = half * HM; i < (half + 1) * HM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[buf][j], fa[i], acc[i][j], 0, FA, 0, (int)wb[j], 0,
+                                                                      (int)wa[i]);
+    } else {
+      if (half == 0) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            xb[j][w] = widen8<E4M3>(fb[buf][j][2 * w], fb[buf][j][2 * w + 1], scale_of(wb[j] & 255u));
+      }
+#pragma unroll
+      for (int i = half * HM; i < (half + 1) * HM; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const bf16x8 xa = widen8<FA>(fa[i][2 * w], fa[i][2 * w + 1], scale_of(wa[i] & 255u));
+#pragma unroll
+          for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[j][w], xa, acc[i][j], 0, 0, 0);
+        }
+    }
+  };
+
+  constexpr int NL = OpA::NL + OpB::NL;
+  words(kt0);
+  auto load_tile = [&](char* S, int t) {
+    oa.load(RA, S, (kt0 + t) * BK);
+    ob.load(RB, S + SB, (kt0 + t) * BK);
+  };
+  load_tile(st0 + grp * STG, 0);
+  load_tile(st1 + grp * STG, 1);
+  load_tile(st2 + grp * STG, 2);
+  wait_vm_lds<2 * NL>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < HM; ++i) fa[i] = oa.frag(st0 + grp * STG, i);
+#pragma unroll
+  for (int j = 0; j < FN; ++j) fb[0][j] = ob.frag(st0 + grp * STG + SB, j);
+
+  // k tile kt is read from stage kt % 4, tile kt + 3 loads into the stage of tile kt - 1
+  auto iter = [&](auto ic, int kt) {
+    constexpr int c = decltype(ic)::value, buf = c & 1;
+    const char* S = stage(std::integral_constant<int, c>());
+    const char* Sn = stage(std::integral_constant<int, c + 1>());
+    char* Sx = stage(std::integral_constant<int, c + 3>());
+    if constexpr (c == 0) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i) wa[i] = na[i];
+#pragma unroll
+      for (int j = 0; j < FN; ++j) wb[j] = nb[j];
+      words(kt0 + kt + 8);
+    } else if constexpr (c % 2 == 0) {  // the next block of 128
+#pragma unroll
+      for (int i = 0; i < FM; ++i) wa[i] >>= 8;
+#pragma unroll
+      for (int j = 0; j < FN; ++j) wb[j] >>= 8;
+    }
+#pragma unroll
+    for (int i = HM; i < FM; ++i) fa[i] = oa.frag(S, i);
+    oa.load(RA, Sx, (kt0 + kt + 3) * BK);
+    mfma_half(0, buf);
+    __builtin_amdgcn_sched_barrier(0);
+    // tile kt + 1 has landed once only the loads of tile kt + 2 and A's of kt + 3 fly
+    wait_vm_lds<NL + OpA::NL>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < HM; ++i) fa[i] = oa.frag(Sn, i);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) fb[buf ^ 1][j] = ob.frag(Sn + SB, j);
+    ob.load(RB, Sx + SB, (kt0 + kt + 3) * BK);
+    mfma_half(1, buf);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  int kt = 0;
+  for (; kt + 7 < nk; kt += 8) {
+    iter(std::integral_constant<int, 0>(), kt);
+    iter(std::integral_constant<int, 1>(), kt + 1);
+    iter(std::integral_constant<int, 2>(), kt + 2);
+    iter(std::integral_constant<int, 3>(), kt + 3);
+    iter(std::integral_constant<int, 4>(), kt + 4);
+    iter(std::integral_constant<int, 5>(), kt + 5);
+    iter(std::integral_constant<int, 6>(), kt + 6);
+    iter(std::integral_constant<int, 7>(), kt + 7);
+  }
+  // the rest: k tiles come in pairs
+  if (kt < nk) {
+    iter(std::integral_constant<int, 0>(), kt);
+    iter(std::integral_constant<int, 1>(), kt + 1);
+  }
+  if (kt + 2 < nk) {
+    iter(std::integral_constant<int, 2>(), kt + 2);
+    iter(std::integral_constant<int, 3>(), kt + 3);
+  }
+  if (kt + 4 < nk) {
+    iter(std::integral_constant<int, 4>(), kt + 4);
+    iter(std::integral_constant<int, 5>(), kt + 5);
+  }
+  // one barrier per k tile: a group with fewer joins the others' rest
+  if constexpr (KG > 1)
+    for (int i = nk; i < nkg; ++i) __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+
+  auto stn = [&](int i) { return i == 0 ? st0 : i == 1 ? st1 : i == 2 ? st2 : st3; };
+  if constexpr (KG > 1) {
+    // the other groups hand theirs to the first, added in group order
+    constexpr int PW = FM * FN * 4096, PER = KG * STG / PW;  // bytes of a wave's sums; waves per stage
+    static_assert(PER >= 1 && NW * (KG - 1) <= 4 * PER, "the sums must fit the stages");
+    if (grp > 0) {
+      const int slot = (grp - 1) * NW + wave;
+      f32x4* const out = (f32x4*)(stn(slot / PER) + slot % PER * PW);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            out[((i * FN + j) * 4 + q) * 64 + lane] =
+                f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    }
+    __syncthreads();
+    if (grp == 0) {
+      for (int o = 0; o < KG - 1; ++o) {
+        const int slot = o * NW + wave;
+        const f32x4* const in = (const f32x4*)(stn(slot / PER) + slot % PER * PW);
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const f32x4 x = in[((i * FN + j) * 4 + q) * 64 + lane];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += x[e];
+            }
+      }
+    }
+    __syncthreads();  // the sums are read: their place is free
+    if (grp > 0) return;
+  }
+
+  // Epilogue: a wave stages 32 rows at a time in its own LDS (it reads back only what
+  // it wrote, in issue order) and stores whole 128-byte lines.
+  constexpr int CS = 32 * FN + 4;  // floats per staged row
+  constexpr int TB = 32 * CS * 4, EPS = KG * STG / TB;  // waves per stage
+  static_assert(EPS >= 1 && NW <= 4 * EPS, "epilogue staging");
+  float* const Ts = (float*)(stn(wave / EPS) + wave % EPS * TB);
+  constexpr int NC = EXACT ? 4 : 8;            // columns per lane and store
+  constexpr int LPR = 32 * FN / NC, RPP = 64 / LPR;  // lanes per row, rows per store
+  const int r_in = lane / LPR, c_in = lane % LPR * NC;
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *(f32x4*)(Ts + l * CS + 32 * j + 8 * q + 4 * h) =
+            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int p = 0; p < 32 / RPP; ++p) {
+      const int r = p * RPP + r_in;
+      float v[NC];
+#pragma unroll
+      for (int q = 0; q < NC / 4; ++q) {
+        const f32x4 x = *(const f32x4*)(Ts + r * CS + c_in + 4 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e];
+      }
+      const int row = m0 + wm * (BM / WM) + 32 * i + r;
+      if (row < M) store_c<T, NC>(g, row, n0 + wn * (BN / WN) + c_in, v);
+    }
+    asm volatile("" ::: "memory");
+  }
+}
+
+template <int FA, typename T, int BM, int BN, int WM, int WN, int KG>
+static void launch_tile(const Matmul8Args& g, hipStream_t s) {
+  const dim3 grid((unsigned)((g.a.rows + BM - 1) / BM) * (unsigned)((g.b.rows + BN - 1) / BN));
+  hipLaunchKernelGGL((matmul8_tile_k<FA, T, BM, BN, WM, WN, KG>), grid, dim3(64 * WM * WN * KG), 0, s, g);
+}
+
+template <int FA, typename T>
 static void launch_matmul8(const Matmul8Args& g, hipStream_t s) {
-  const dim3 grid((unsigned)((g.a.rows + 63) / 64) * (unsigned)((g.b.rows + 63) / 64));
-  if (g.out_dt == BF16) hipLaunchKernelGGL((matmul8_k<FA, uint16_t>), grid, dim3(256), 0, s, g);
-  else hipLaunchKernelGGL((matmul8_k<FA, float>), grid, dim3(256), 0, s, g);
+  const long t256 = (long)((g.a.rows + 255) / 256) * ((g.b.rows + 255) / 256);
+  const long t128 = (long)((g.a.rows + 127) / 128) * ((g.b.rows + 127) / 128);
+  if (t256 >= 128) launch_tile<FA, T, 256, 256, 2, 4, 1>(g, s);
+  else if (t128 >= 128) launch_tile<FA, T, 128, 128, 2, 2, 1>(g, s);
+  else launch_tile<FA, T, 64, 64, 1, 2, 4>(g, s);
 }
 
 int matmul8(const Matmul8Args& g, hipStream_t s) {
-  if (g.a.fmt == E5M2) launch_matmul8<1>(g, s);
-  else launch_matmul8<0>(g, s);
+  if (g.out_dt == BF16) {
+    if (g.a.fmt == E5M2) launch_matmul8<E5M2, uint16_t>(g, s);
+    else launch_matmul8<E4M3, uint16_t>(g, s);
+  } else {
+    if (g.a.fmt == E5M2) launch_matmul8<E5M2, float>(g, s);
+    else launch_matmul8<E4M3, float>(g, s);
+  }
   JG_CHECK_LAUNCH("matmul8");
   return 0;
 }
