@@ -392,6 +392,236 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void matmul8_tile_k(Matmul8Args 
   }
 }
 
+// ------------------------------------------------------- tiled kernel, 128 deep
+// BM x BN tiles for bf16 results, four waves of (BM / 2) x (BN / 2) made of 32 x 32
+// fragments, k tiles of 128 bytes (one block) through two LDS stages.  One wave per
+// SIMD holds its part of C in 256 accumulator registers and reads (128 + 128) x 128
+// bytes for 64 instructions, two thirds of what eight waves of 128 x 64 read: the card
+// runs at its power limit here, and what LDS reads do not take, the clock gets.
+//
+// With one wave per SIMD nothing hides a wait, so every LDS read and direct load is
+// issued a quarter of a k tile or more before its use.  A k tile is four quarters,
+// (half of A) x (half of B); halves of A and B are named 0 and 1, and Bp is B's half p,
+// p = the k tile's parity:
+//   quarter 0: A0 Bp       while B(1-p) is read
+//   quarter 1: A0 B(1-p)   while A1 is read; barrier: the stage is read by all
+//   quarter 2: A1 B(1-p)   while half of k tile + 2 is loaded into that stage;
+//                          barrier: the next k tile has landed
+//   quarter 3: A1 Bp       while the other half is loaded and the next k tile's A0
+//                          and B(1-p) are read: its first quarter's operands
+// LDS rows are 128 bytes; chunk c (16 bytes) of row r lies at c ^ ((r >> 1) & 7): a
+// read's 16 neighbouring lanes (16 rows, one chunk), and groups such as {0-3, 32-35},
+// then cover the 64 banks once (with c ^ (r & 7) the counters showed 4 conflict cycles
+// a read).
+template <int ROWS, int WR>
+struct Op8q {
+  static constexpr int NL = ROWS / 32;  // direct loads of 1 KB (8 rows) per wave and k tile
+  static_assert(NL % 2 == 0, "a load's parity is its rows' bit 3");
+  int voff, step;                       // offset of the first; bytes from one to the next
+  int fo;                               // chunk 4 h of this lane's row of fragment 0; chunk 4 h + x lies at fo ^ 16 x
+  __device__ inline void init(int ld, int wrow0) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    voff = (8 * wave * NL + lane / 8) * ld + 16 * ((lane & 7) ^ (lane >> 4));
+    step = 8 * ld;
+    const int r = lane & 31;
+    fo = (wrow0 + r) * 128 + ((4 * (lane >> 5)) ^ ((r >> 1) & 7)) * 16;
+  }
+  // loads t0 .. t0 + n - 1 of the k tile at k0 into the stage at S
+  template <int T0, int N>
+  __device__ inline void load(__amdgpu_buffer_rsrc_t R, char* S, int k0) const {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int t = T0; t < T0 + N; ++t) load_lds16(R, S + (wave * NL + t) * 1024, (t & 1 ? voff ^ 64 : voff) + (t * step + k0));
+  }
+  __device__ inline i32x8 frag(const char* S, int i, int kk) const {
+    const i32x4 a = *(const i32x4*)(S + (fo ^ (32 * kk)) + i * 4096), b = *(const i32x4*)(S + (fo ^ (32 * kk + 16)) + i * 4096);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+};
+
+template <int FA, int BM, int BN, int L2, int L3>
+__global__ __launch_bounds__(256) void matmul8_quad_k(Matmul8Args g) {
+  constexpr int BK = 128, SM = BM / 64, SN = BN / 64, HM = SM / 2, HN = SN / 2;  // 32 x 32 fragments of a wave
+  constexpr int SB = BM * BK;
+  __shared__ __attribute__((aligned(1024))) char st0[(BM + BN) * BK];
+  __shared__ __attribute__((aligned(1024))) char st1[(BM + BN) * BK];
+
+  const int M = g.a.rows, N = g.b.rows;
+  const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
+  int tm, tn;
+  tile_coords(xcd_remap(blockIdx.x, tiles_m * tiles_n), tiles_m, tiles_n, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN;
+  const int lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
+
+  typedef Op8q<BM, BM / 2> OpA;
+  typedef Op8q<BN, BN / 2> OpB;
+  OpA oa;
+  OpB ob;
+  oa.init((int)g.a.ld, wm * (BM / 2));
+  ob.init((int)g.b.ld, wn * (BN / 2));
+  // the tile's rows: offsets stay below 2^31 (ld <= 2^22), rows past the end and the
+  // prefetch behind the last row read zeros
+  const int nk = (g.a.k + BK - 1) / BK;
+  const __amdgpu_buffer_rsrc_t RA = make_rsrc(g.a.q + (size_t)m0 * g.a.ld, (min(BM, M - m0) - 1) * (long)g.a.ld + nk * BK);
+  const __amdgpu_buffer_rsrc_t RB = make_rsrc(g.b.q + (size_t)n0 * g.b.ld, (min(BN, N - n0) - 1) * (long)g.b.ld + nk * BK);
+
+  // exponent words of the tile's rows, four k tiles each: through LDS as well
+  __shared__ __attribute__((aligned(256))) uint32_t stw[BM + BN];
+  uint32_t wa[SM], wb[SN];
+  auto load_words = [&](int t) {  // of k tile t (a multiple of 4); the last ones again behind the end
+    const size_t w = min(t, nk - 1) / 4;
+    const __amdgpu_buffer_rsrc_t WA = make_rsrc(g.a.sc + w * M + m0, min(BM, M - m0) * 4);
+    const __amdgpu_buffer_rsrc_t WB = make_rsrc(g.b.sc + w * N + n0, min(BN, N - n0) * 4);
+#pragma unroll
+    for (int i = 0; i < BM / 256; ++i) load_lds4(WA, (char*)(stw + i * 256 + wave * 64), (i * 256 + (int)threadIdx.x) * 4);
+#pragma unroll
+    for (int i = 0; i < BN / 256; ++i) load_lds4(WB, (char*)(stw + BM + i * 256 + wave * 64), (i * 256 + (int)threadIdx.x) * 4);
+  };
+  constexpr int NWL = BM / 256 + BN / 256;  // direct loads of words per wave
+
+  f32x16 acc[SM][SN];
+#pragma unroll
+  for (int i = 0; i < SM; ++i)
+#pragma unroll
+    for (int j = 0; j < SN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  i32x8 fa[SM][2], fb[SN][2];
+  auto read_a = [&](const char* S, int half, bool w) {  // w: the exponent words too
+#pragma unroll
+    for (int i = half * HM; i < (half + 1) * HM; ++i) {
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) fa[i][kk] = oa.frag(S, i, kk);
+      if (w) wa[i] = stw[wm * (BM / 2) + 32 * i + l];
+    }
+  };
+  auto read_b = [&](const char* S, int half, bool w) {
+#pragma unroll
+    for (int j = half * HN; j < (half + 1) * HN; ++j) {
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) fb[j][kk] = ob.frag(S + SB, j, kk);
+      if (w) wb[j] = stw[BM + wn * (BN / 2) + 32 * j + l];
+    }
+  };
+  auto quarter = [&](auto cc, int ah, int bh) {  // cc: byte of the exponent words
+    constexpr int c = decltype(cc)::value;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int i = ah * HM; i < (ah + 1) * HM; ++i)
+#pragma unroll
+        for (int j = bh * HN; j < (bh + 1) * HN; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[j][kk], fa[i][kk], acc[i][j], 0, FA, c, (int)wb[j], c,
+                                                                      (int)wa[i]);
+  };
+
+  // direct loads LO .. HI - 1 of k tile t (A's, then B's)
+  auto load = [&](auto lo, auto hi, char* S, int t) {
+    constexpr int LO = decltype(lo)::value, HI = decltype(hi)::value, NA = OpA::NL;
+    if constexpr (LO < NA) oa.template load<LO, (HI < NA ? HI : NA) - LO>(RA, S, t * BK);
+    if constexpr (HI > NA) ob.template load<(LO > NA ? LO - NA : 0), HI - (LO > NA ? LO : NA)>(RB, S + SB, t * BK);
+  };
+  constexpr int NL = OpA::NL + OpB::NL;
+  typedef std::integral_constant<int, 0> C0;
+  typedef std::integral_constant<int, NL * L2 / 16> C1;
+  typedef std::integral_constant<int, NL * (L2 + L3) / 16> C2;
+  typedef std::integral_constant<int, NL> C3;
+  load_words(0);
+  load(C0(), C3(), st0, 0);
+  load(C0(), C2(), st1, 1);
+  wait_vm_lds<C2::value>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  read_a(st0, 0, true);
+  read_b(st0, 0, true);
+
+  constexpr int MF = 2 * HM * HN;
+  auto iter = [&](auto cc, int kt) {
+    constexpr int c = decltype(cc)::value, p = c & 1;
+    char* S = p ? st1 : st0;
+    const char* Sn = p ? st0 : st1;
+    // keeps the fragments' addresses (too far apart for one base) from being held in
+    // registers over the loop: an addition each instead
+    asm("" : "+v"(oa.fo), "+v"(ob.fo));
+    read_b(S, 1 - p, c == 0);
+    load(C2(), C3(), p ? st0 : st1, kt + 1);
+    quarter(cc, 0, p);
+    pipe_sched<MF, (c == 0 ? 5 : 4) * HN, 0, NL - C2::value>();
+    __builtin_amdgcn_sched_barrier(0);
+    read_a(S, 1, c == 0);
+    quarter(cc, 0, 1 - p);
+    pipe_sched<MF, (c == 0 ? 5 : 4) * HM, 0, 0>();
+    __builtin_amdgcn_sched_barrier(0);
+    // every wave's reads of this stage are done
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    // (the words of the four k tiles under way are in registers since the first of them)
+    if constexpr (c == 1) load_words(kt + 3);
+    load(C0(), C1(), S, kt + 2);
+    quarter(cc, 1, 1 - p);
+    pipe_sched<MF, 0, 0, C1::value + (c == 1 ? NWL : 0)>();
+    __builtin_amdgcn_sched_barrier(0);
+    // the next k tile has landed once only this quarter's loads fly
+    wait_vm_lds<C1::value + (c == 1 ? NWL : 0)>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    load(C1(), C2(), S, kt + 2);
+    read_a(Sn, 0, c == 3);
+    read_b(Sn, 1 - p, c == 3);
+    quarter(cc, 1, p);
+    pipe_sched<MF, (c == 3 ? 5 : 4) * (HM + HN), 0, C2::value - C1::value>();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  int kt = 0;
+  for (; kt + 3 < nk; kt += 4) {
+    iter(std::integral_constant<int, 0>(), kt);
+    iter(std::integral_constant<int, 1>(), kt + 1);
+    iter(std::integral_constant<int, 2>(), kt + 2);
+    iter(std::integral_constant<int, 3>(), kt + 3);
+  }
+  if (kt < nk) iter(std::integral_constant<int, 0>(), kt);
+  if (kt + 1 < nk) iter(std::integral_constant<int, 1>(), kt + 1);
+  if (kt + 2 < nk) iter(std::integral_constant<int, 2>(), kt + 2);
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+
+  // Epilogue: a wave stages 32 rows at a time in its own LDS (it reads back only what
+  // it wrote, in issue order) and stores whole lines of its columns.
+  constexpr int CS = BN / 2 + 4;  // floats per staged row
+  static_assert(2 * 32 * CS * 4 <= (BM + BN) * BK, "epilogue staging");
+  float* const Ts = (float*)((wave & 2 ? st1 : st0) + (wave & 1) * (32 * CS * 4));
+  constexpr int LPR = BN / 2 / 8, RPP = 64 / LPR;  // lanes per row, rows per store
+  const int r_in = lane / LPR, c_in = lane % LPR * 8;
+#pragma unroll
+  for (int i = 0; i < SM; ++i) {
+#pragma unroll
+    for (int j = 0; j < SN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *(f32x4*)(Ts + l * CS + 32 * j + 8 * q + 4 * h) =
+            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int p = 0; p < 32 / RPP; ++p) {
+      const int r = p * RPP + r_in;
+      float v[8];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const f32x4 x = *(const f32x4*)(Ts + r * CS + c_in + 4 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e];
+      }
+      const int row = m0 + wm * (BM / 2) + 32 * i + r;
+      if (row < M) store_c<uint16_t, 8>(g, row, n0 + wn * (BN / 2) + c_in, v);
+    }
+    asm volatile("" ::: "memory");
+  }
+}
+
 template <int FA, typename T, int BM, int BN, int WM, int WN, int KG>
 static void launch_tile(const Matmul8Args& g, hipStream_t s) {
   const dim3 grid((unsigned)((g.a.rows + BM - 1) / BM) * (unsigned)((g.b.rows + BN - 1) / BN));
@@ -402,7 +632,10 @@ template <int FA, typename T>
 static void launch_matmul8(const Matmul8Args& g, hipStream_t s) {
   const long t256 = (long)((g.a.rows + 255) / 256) * ((g.b.rows + 255) / 256);
   const long t128 = (long)((g.a.rows + 127) / 128) * ((g.b.rows + 127) / 128);
-  if (t256 >= 128) launch_tile<FA, T, 256, 256, 2, 4, 1>(g, s);
+  if (t256 >= 128) {
+    if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((matmul8_quad_k<FA, 256, 256, 6, 5>), dim3((unsigned)t256), dim3(256), 0, s, g);
+    else launch_tile<FA, T, 256, 256, 2, 4, 1>(g, s);
+  }
   else if (t128 >= 128) launch_tile<FA, T, 128, 128, 2, 2, 1>(g, s);
   else launch_tile<FA, T, 64, 64, 1, 2, 4>(g, s);
 }

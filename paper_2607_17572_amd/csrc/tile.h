@@ -32,6 +32,10 @@ __device__ inline __amdgpu_buffer_rsrc_t make_rsrc(const void* p, long bytes) {
 __device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t R, char* S, int off) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(R, JG_LDS(S), 16, off, 0, 0, 0);
 }
+// 4 bytes per lane into 256 bytes
+__device__ __forceinline__ void load_lds4(__amdgpu_buffer_rsrc_t R, char* S, int off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(R, JG_LDS(S), 4, off, 0, 0, 0);
+}
 
 // First half of the workgroup barrier for the direct-loaded stages: this
 // wave's LDS reads done (lgkmcnt 0) and at most NV of its direct loads still
