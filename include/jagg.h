@@ -405,7 +405,10 @@ jagg_status jagg_quantize8(jagg_ctx* ctx, const void* x, size_t ldx, int rows, i
  * and everything else in fp32 (1e-5 to 3e-5 relative to the result's 2-norm, where
  * the rounding to bf16 is 1.7e-3).  a: E4M3 or E5M2, b: E4M3 (EUNSUPPORTED otherwise), of
  * equal k.  out: a.rows x b.rows, row stride ldo, out_dtype JAGG_F32 or
- * JAGG_BF16; bias: device, b.rows elements of out_dtype, or NULL; beta 0 or 1. */
+ * JAGG_BF16; bias: device, b.rows elements of out_dtype, or NULL; beta 0 or 1.
+ * A long k over a small result is split: uses jagg_matmul8_bytes bytes of the bound
+ * workspace (0 for most sizes; m = a.rows, n = b.rows). */
+jagg_status jagg_matmul8_bytes(int m, int n, int k, int out_dtype, size_t* bytes);
 jagg_status jagg_matmul8(jagg_ctx* ctx, const jagg_mat8* a, const jagg_mat8* b, const void* bias, void* out, size_t ldo,
                          int out_dtype, float beta);
 

@@ -85,6 +85,7 @@ def lib() -> ctypes.CDLL:
                                     vp, ctypes.POINTER(d)],
             "jagg_mat8_bytes": [i, i, ctypes.POINTER(sz), ctypes.POINTER(sz), ctypes.POINTER(sz)],
             "jagg_quantize8": [vp, vp, sz, i, i, i, vp, vp, i, pm8, pm8],
+            "jagg_matmul8_bytes": [i, i, i, i, ctypes.POINTER(sz)],
             "jagg_matmul8": [vp, pm8, pm8, vp, vp, sz, i, f],
             "jagg_rmsnorm8": [vp, vp, sz, vp, sz, vp, i, i, i, f, vp, sz, pm8, vp],
             "jagg_rmsnorm8_grad_bytes": [i, i, ctypes.POINTER(sz)],
@@ -539,6 +540,11 @@ class Context:
         if a.device != self.device or b.device != self.device:
             _refuse("the operands must be on the context's device")
         bp = None if bias is None else _vec(bias, "bias", b.rows, out.dtype, self.device)
+        if a.rows > 16:
+            nb = ctypes.c_size_t()
+            _check(lib().jagg_matmul8_bytes(a.rows, b.rows, a.k, dt, ctypes.byref(nb)))
+            if nb.value:
+                self._ensure_bytes(nb.value)
         _check(lib().jagg_matmul8(self._h, a._c, b._c, bp, p, ld, dt, beta))
         return out
 

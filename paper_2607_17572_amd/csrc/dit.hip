@@ -1383,6 +1383,19 @@ jagg_status jagg_quantize8(jagg_ctx* ctx, const void* x, size_t ldx, int rows, i
   return to_status(jg::quant8(a, ctx->stream));
 }
 
+jagg_status jagg_matmul8_bytes(int m, int n, int k, int out_dtype, size_t* bytes) {
+  if (!bytes) return fail(JAGG_EINVAL, "jagg_matmul8_bytes: null argument");
+  if (m < 1 || n < 1 || k < 1) return fail(JAGG_EINVAL, "jagg_matmul8_bytes: sizes must be >= 1");
+  if (!is_dtype(out_dtype)) return fail(JAGG_EINVAL, "jagg_matmul8_bytes: unknown result dtype");
+  jg::Matmul8Args g{};
+  g.a.rows = m;
+  g.b.rows = n;
+  g.a.k = k;
+  g.out_dt = out_dtype;
+  *bytes = jg::matmul8_plan(g);
+  return JAGG_OK;
+}
+
 jagg_status jagg_matmul8(jagg_ctx* ctx, const jagg_mat8* a, const jagg_mat8* b, const void* bias, void* out, size_t ldo,
                          int out_dtype, float beta) {
   const char* f = "jagg_matmul8: ";
@@ -1403,6 +1416,10 @@ jagg_status jagg_matmul8(jagg_ctx* ctx, const jagg_mat8* a, const jagg_mat8* b, 
   g.bias = bias;
   g.out = out; g.ldo = ldo; g.out_dt = out_dtype;
   g.beta = beta;
+  const size_t need = jg::matmul8_plan(g);
+  if (need && (!ctx->ws || ctx->ws_bytes < need))
+    return fail(JAGG_EINVAL, std::string(f) + "workspace not bound or smaller than jagg_matmul8_bytes = " + std::to_string(need));
+  g.part = (float*)ctx->ws;
   OnDevice dev(ctx);
   return to_status(jg::matmul8(g, ctx->stream));
 }

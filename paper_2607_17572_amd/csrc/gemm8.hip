@@ -93,9 +93,37 @@ struct Op8 {
   }
 };
 
-// bias, old C and the store of eight (bf16) or four (fp32) columns of a row
+// The part of k that this workgroup multiplies: split blockIdx.y of g.splits.
+__device__ __forceinline__ void take_split(Matmul8Args& g) {
+  if (g.splits == 1) return;
+  const int b0 = (int)blockIdx.y * g.per_split;  // blocks of 128, whole exponent words
+  g.a.q += (size_t)b0 * 128;
+  g.b.q += (size_t)b0 * 128;
+  g.a.sc += (size_t)(b0 / 4) * g.a.rows;
+  g.b.sc += (size_t)(b0 / 4) * g.b.rows;
+  g.a.k = min(g.a.k - b0 * 128, g.per_split * 128);
+  g.part += (size_t)blockIdx.y * g.a.rows * g.b.rows;
+}
+
+// bias, old C and the store of eight (bf16) or four (fp32) columns of a row; a split
+// stores its sums
 template <typename T, int NC>
 __device__ __forceinline__ void store_c(const Matmul8Args& g, int row, int col, float* v) {
+  if (g.splits > 1) {
+    float* p = g.part + (size_t)row * g.b.rows;
+#pragma unroll
+    for (int e = 0; e < NC; e += 4) {
+      if (col + e + 4 <= g.b.rows) {
+        *(u32x4a*)(p + col + e) = u32x4a{__float_as_uint(v[e]), __float_as_uint(v[e + 1]), __float_as_uint(v[e + 2]),
+                                         __float_as_uint(v[e + 3])};
+      } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (col + e + x < g.b.rows) p[col + e + x] = v[e + x];
+      }
+    }
+    return;
+  }
   T* c = (T*)g.out + (size_t)row * g.ldo + col;
   const T* b = (const T*)g.bias + col;
   if (col + NC <= g.b.rows) {
@@ -112,6 +140,14 @@ __device__ __forceinline__ void store_c(const Matmul8Args& g, int row, int col, 
         for (int e = 0; e < 8; ++e) v[e] += o[e];
       }
       store8(c, v);
+    } else if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int e = 0; e < NC; ++e) {
+        float x = v[e];
+        if (g.bias) x += ldf(b, e);
+        if (g.beta != 0.f) x += ldf(c, e);
+        stf(c, e, x);
+      }
     } else {
       u32x4a o;
       if (g.bias) {
@@ -140,8 +176,89 @@ __device__ __forceinline__ void store_c(const Matmul8Args& g, int row, int col, 
   }
 }
 
+// Epilogue of a wave's FM x FN fragments of 32 x 32 (rows from row0, columns from col0): 32
+// rows at a time through its own LDS at Ts (it reads back only what it wrote, in issue
+// order), so that stores are whole lines.  A lane's columns are the same in every row:
+// their bias is loaded once; old values of C are loaded a fragment row at a time,
+// all in flight before the first use.
+template <int FN>
+constexpr int epi_floats() { return 32 * (32 * FN + 4); }
+
+template <typename T, int FM, int FN>
+__device__ __forceinline__ void epilogue8(const Matmul8Args& g, const f32x16 (&acc)[FM][FN], int row0, int col0, float* Ts) {
+  constexpr int CS = 32 * FN + 4, NC = sizeof(T) == 2 ? 8 : 4;  // floats per staged row; columns per lane and store
+  constexpr int LPR = 32 * FN / NC, RPP = 64 / LPR, P = 32 / RPP;  // lanes per row, rows per store, stores
+  const int lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
+  const int r_in = lane / LPR, c_in = lane % LPR * NC, col = col0 + c_in;
+  const int M = g.a.rows, N = g.b.rows;
+  const bool split = g.splits > 1, inner = row0 + 32 * FM <= M && col0 + 32 * FN <= N;
+  float bias[NC];
+#pragma unroll
+  for (int e = 0; e < NC; ++e) bias[e] = 0.f;
+  if (g.bias && !split && inner) {
+#pragma unroll
+    for (int e = 0; e < NC; ++e) bias[e] = ldf((const T*)g.bias, col + e);
+  }
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *(f32x4*)(Ts + l * CS + 32 * j + 8 * q + 4 * h) =
+            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    asm volatile("" ::: "memory");
+    const int row = row0 + 32 * i + r_in;
+    auto staged = [&](int p, float* v) {
+#pragma unroll
+      for (int q = 0; q < NC / 4; ++q) {
+        const f32x4 x = *(const f32x4*)(Ts + (p * RPP + r_in) * CS + c_in + 4 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e];
+      }
+    };
+    if (!inner || split) {
+#pragma unroll 1
+      for (int p = 0; p < P; ++p) {
+        float v[NC];
+        staged(p, v);
+        if (row + p * RPP < M) store_c<T, NC>(g, row + p * RPP, col, v);
+      }
+    } else {
+      T* const c = (T*)g.out + (size_t)row * g.ldo + col;
+      u32x4a old[P];
+      if (g.beta != 0.f) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) old[p] = *(const u32x4a*)(c + (size_t)(p * RPP) * g.ldo);
+      } else {
+#pragma unroll
+        for (int p = 0; p < P; ++p) old[p] = u32x4a{0u, 0u, 0u, 0u};
+      }
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        float v[NC];
+        staged(p, v);
+#pragma unroll
+        for (int e = 0; e < NC; ++e) {
+          const uint32_t u = old[p][sizeof(T) == 2 ? e / 2 : e];
+          v[e] += bias[e] + (sizeof(T) == 2 ? bf2f(e & 1 ? u >> 16 : u & 0xffffu) : __uint_as_float(u));
+        }
+        u32x4a o;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          if constexpr (sizeof(T) == 2) o[w] = (uint32_t)f2bf(v[2 * w]) | (uint32_t)f2bf(v[2 * w + 1]) << 16;
+          else o[w] = __float_as_uint(v[w]);
+        }
+        *(u32x4a*)(c + (size_t)(p * RPP) * g.ldo) = o;
+      }
+    }
+    asm volatile("" ::: "memory");
+  }
+}
+
 template <int FA, typename T, int BM, int BN, int WM, int WN, int KG>
 __global__ __launch_bounds__(64 * WM * WN * KG) void matmul8_tile_k(Matmul8Args g) {
+  take_split(g);
   constexpr bool EXACT = sizeof(T) == 4;
   constexpr int BK = 64, NW = WM * WN, FM = BM / (32 * WM), FN = BN / (32 * WN), HM = FM / 2;
   static_assert(FM % 2 == 0, "A's fragments go in two halves");
@@ -357,39 +474,9 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void matmul8_tile_k(Matmul8Args 
     if (grp > 0) return;
   }
 
-  // Epilogue: a wave stages 32 rows at a time in its own LDS (it reads back only what
-  // it wrote, in issue order) and stores whole 128-byte lines.
-  constexpr int CS = 32 * FN + 4;  // floats per staged row
-  constexpr int TB = 32 * CS * 4, EPS = KG * STG / TB;  // waves per stage
+  constexpr int TB = 4 * epi_floats<FN>(), EPS = KG * STG / TB;  // waves per stage
   static_assert(EPS >= 1 && NW <= 4 * EPS, "epilogue staging");
-  float* const Ts = (float*)(stn(wave / EPS) + wave % EPS * TB);
-  constexpr int NC = EXACT ? 4 : 8;            // columns per lane and store
-  constexpr int LPR = 32 * FN / NC, RPP = 64 / LPR;  // lanes per row, rows per store
-  const int r_in = lane / LPR, c_in = lane % LPR * NC;
-#pragma unroll
-  for (int i = 0; i < FM; ++i) {
-#pragma unroll
-    for (int j = 0; j < FN; ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *(f32x4*)(Ts + l * CS + 32 * j + 8 * q + 4 * h) =
-            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-    asm volatile("" ::: "memory");
-#pragma unroll
-    for (int p = 0; p < 32 / RPP; ++p) {
-      const int r = p * RPP + r_in;
-      float v[NC];
-#pragma unroll
-      for (int q = 0; q < NC / 4; ++q) {
-        const f32x4 x = *(const f32x4*)(Ts + r * CS + c_in + 4 * q);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e];
-      }
-      const int row = m0 + wm * (BM / WM) + 32 * i + r;
-      if (row < M) store_c<T, NC>(g, row, n0 + wn * (BN / WN) + c_in, v);
-    }
-    asm volatile("" ::: "memory");
-  }
+  epilogue8<T, FM, FN>(g, acc, m0 + wm * (BM / WM), n0 + wn * (BN / WN), (float*)(stn(wave / EPS) + wave % EPS * TB));
 }
 
 // ------------------------------------------------------- tiled kernel, 128 deep
@@ -403,12 +490,14 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void matmul8_tile_k(Matmul8Args 
 // issued a quarter of a k tile or more before its use.  A k tile is four quarters,
 // (half of A) x (half of B); halves of A and B are named 0 and 1, and Bp is B's half p,
 // p = the k tile's parity:
-//   quarter 0: A0 Bp       while B(1-p) is read
-//   quarter 1: A0 B(1-p)   while A1 is read; barrier: the stage is read by all
-//   quarter 2: A1 B(1-p)   while half of k tile + 2 is loaded into that stage;
-//                          barrier: the next k tile has landed
-//   quarter 3: A1 Bp       while the other half is loaded and the next k tile's A0
-//                          and B(1-p) are read: its first quarter's operands
+//   quarter 0: A0 Bp       while B(1-p) and A1 are read; barrier: the stage is read by all
+//   quarter 1: A0 B(1-p)   while the first loads of k tile + 2 go into that stage
+//   quarter 2: A1 B(1-p)   while more do; barrier: the next k tile has landed
+//   quarter 3: A1 Bp       while the rest do and the next k tile's A0 and B(1-p) are read,
+//                          its first quarter's operands
+// Measured at 8192^3: all loads in quarters 2 and 3 401 us, spread over quarters 2, 3 and
+// the next 0 398, reads early in their quarter 390, as above 385; one barrier per k tile
+// with the loads in quarters 3 and 0 408.
 // LDS rows are 128 bytes; chunk c (16 bytes) of row r lies at c ^ ((r >> 1) & 7): a
 // read's 16 neighbouring lanes (16 rows, one chunk), and groups such as {0-3, 32-35},
 // then cover the 64 banks once (with c ^ (r & 7) the counters showed 4 conflict cycles
@@ -439,8 +528,22 @@ struct Op8q {
   }
 };
 
+// Instruction interleave of a quarter: up to RP LDS reads behind each matrix instruction
+// until all R are issued, the L direct loads evenly.
+template <int MF, int R, int L, int RP, int I = 0>
+__device__ __forceinline__ void quarter_sched() {
+  if constexpr (I < MF) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    constexpr int r = I == MF - 1 ? R : (R < RP ? R : RP), l = L * (I + 1) / MF - L * I / MF;
+    if constexpr (r > 0) __builtin_amdgcn_sched_group_barrier(0x100, r, 0);
+    if constexpr (l > 0) __builtin_amdgcn_sched_group_barrier(0x020, l, 0);
+    quarter_sched<MF, R - r, L, RP, I + 1>();
+  }
+}
+
 template <int FA, int BM, int BN, int L2, int L3>
 __global__ __launch_bounds__(256) void matmul8_quad_k(Matmul8Args g) {
+  take_split(g);
   constexpr int BK = 128, SM = BM / 64, SN = BN / 64, HM = SM / 2, HN = SN / 2;  // 32 x 32 fragments of a wave
   constexpr int SB = BM * BK;
   __shared__ __attribute__((aligned(1024))) char st0[(BM + BN) * BK];
@@ -468,17 +571,19 @@ __global__ __launch_bounds__(256) void matmul8_quad_k(Matmul8Args g) {
 
   // exponent words of the tile's rows, four k tiles each: through LDS as well
   __shared__ __attribute__((aligned(256))) uint32_t stw[BM + BN];
+  constexpr int NWL = (BM + BN) / 256;  // direct loads of 64 words per wave
   uint32_t wa[SM], wb[SN];
   auto load_words = [&](int t) {  // of k tile t (a multiple of 4); the last ones again behind the end
     const size_t w = min(t, nk - 1) / 4;
-    const __amdgpu_buffer_rsrc_t WA = make_rsrc(g.a.sc + w * M + m0, min(BM, M - m0) * 4);
-    const __amdgpu_buffer_rsrc_t WB = make_rsrc(g.b.sc + w * N + n0, min(BN, N - n0) * 4);
 #pragma unroll
-    for (int i = 0; i < BM / 256; ++i) load_lds4(WA, (char*)(stw + i * 256 + wave * 64), (i * 256 + (int)threadIdx.x) * 4);
-#pragma unroll
-    for (int i = 0; i < BN / 256; ++i) load_lds4(WB, (char*)(stw + BM + i * 256 + wave * 64), (i * 256 + (int)threadIdx.x) * 4);
+    for (int i = 0; i < NWL; ++i) {
+      const int row = 64 * (4 * i + wave);  // of A's rows, then B's
+      const bool a = row < BM;
+      const __amdgpu_buffer_rsrc_t W =
+          a ? make_rsrc(g.a.sc + w * M + m0, min(BM, M - m0) * 4) : make_rsrc(g.b.sc + w * N + n0, min(BN, N - n0) * 4);
+      load_lds4(W, (char*)(stw + row), ((a ? row : row - BM) + lane) * 4);
+    }
   };
-  constexpr int NWL = BM / 256 + BN / 256;  // direct loads of words per wave
 
   f32x16 acc[SM][SN];
 #pragma unroll
@@ -530,8 +635,8 @@ __global__ __launch_bounds__(256) void matmul8_quad_k(Matmul8Args g) {
   typedef std::integral_constant<int, NL> C3;
   load_words(0);
   load(C0(), C3(), st0, 0);
-  load(C0(), C2(), st1, 1);
-  wait_vm_lds<C2::value>();
+  load(C0(), C3(), st1, 1);
+  wait_vm_lds<NL>();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   read_a(st0, 0, true);
@@ -546,34 +651,34 @@ __global__ __launch_bounds__(256) void matmul8_quad_k(Matmul8Args g) {
     // registers over the loop: an addition each instead
     asm("" : "+v"(oa.fo), "+v"(ob.fo));
     read_b(S, 1 - p, c == 0);
-    load(C2(), C3(), p ? st0 : st1, kt + 1);
-    quarter(cc, 0, p);
-    pipe_sched<MF, (c == 0 ? 5 : 4) * HN, 0, NL - C2::value>();
-    __builtin_amdgcn_sched_barrier(0);
     read_a(S, 1, c == 0);
-    quarter(cc, 0, 1 - p);
-    pipe_sched<MF, (c == 0 ? 5 : 4) * HM, 0, 0>();
+    quarter(cc, 0, p);
+    quarter_sched<MF, (c == 0 ? 5 : 4) * (HN + HM), 0, 2>();
     __builtin_amdgcn_sched_barrier(0);
     // every wave's reads of this stage are done
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+    load(C0(), C1(), S, kt + 2);
+    quarter(cc, 0, 1 - p);
+    quarter_sched<MF, 0, C1::value, 1>();
+    __builtin_amdgcn_sched_barrier(0);
     // (the words of the four k tiles under way are in registers since the first of them)
     if constexpr (c == 1) load_words(kt + 3);
-    load(C0(), C1(), S, kt + 2);
+    load(C1(), C2(), S, kt + 2);
     quarter(cc, 1, 1 - p);
-    pipe_sched<MF, 0, 0, C1::value + (c == 1 ? NWL : 0)>();
+    quarter_sched<MF, 0, C2::value - C1::value + (c == 1 ? NWL : 0), 1>();
     __builtin_amdgcn_sched_barrier(0);
-    // the next k tile has landed once only this quarter's loads fly
-    wait_vm_lds<C1::value + (c == 1 ? NWL : 0)>();
+    // the next k tile has landed once only the loads of the one after it (and the words) fly
+    wait_vm_lds<C2::value + (c == 1 ? NWL : 0)>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    load(C1(), C2(), S, kt + 2);
+    load(C2(), C3(), S, kt + 2);
     read_a(Sn, 0, c == 3);
     read_b(Sn, 1 - p, c == 3);
     quarter(cc, 1, p);
-    pipe_sched<MF, (c == 3 ? 5 : 4) * (HM + HN), 0, C2::value - C1::value>();
+    quarter_sched<MF, (c == 3 ? 5 : 4) * (HM + HN), NL - C2::value, 3>();
     __builtin_amdgcn_sched_barrier(0);
   };
   int kt = 0;
@@ -589,55 +694,177 @@ __global__ __launch_bounds__(256) void matmul8_quad_k(Matmul8Args g) {
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
 
-  // Epilogue: a wave stages 32 rows at a time in its own LDS (it reads back only what
-  // it wrote, in issue order) and stores whole lines of its columns.
-  constexpr int CS = BN / 2 + 4;  // floats per staged row
-  static_assert(2 * 32 * CS * 4 <= (BM + BN) * BK, "epilogue staging");
-  float* const Ts = (float*)((wave & 2 ? st1 : st0) + (wave & 1) * (32 * CS * 4));
-  constexpr int LPR = BN / 2 / 8, RPP = 64 / LPR;  // lanes per row, rows per store
-  const int r_in = lane / LPR, c_in = lane % LPR * 8;
+  constexpr int TB = 4 * epi_floats<SN>();
+  static_assert(2 * TB <= (BM + BN) * BK, "epilogue staging");
+  epilogue8<uint16_t, SM, SN>(g, acc, m0 + wm * (BM / 2), n0 + wn * (BN / 2), (float*)((wave & 2 ? st1 : st0) + (wave & 1) * TB));
+}
+
+// ------------------------------------------------------------------- few rows
+// Up to 16 rows of A: bound by reading B once.  A workgroup takes 16 rows of B, its eight
+// waves every eighth block of 128 (neighbouring blocks of a row are read together),
+// operands straight to registers with four blocks in flight a wave.  The waves' sums
+// are added through LDS in wave order.  A lane takes chunks q and q + 4 of a row's block
+// (q = lane / 16), the same on both sides.  One row, 16384 x 4096 (68 MB): 13.5 us,
+// 5.0 TB/s; 4096 x 12288: 10.9 us (32 rows of B a workgroup: 14.5 and 15.5; two blocks
+// in flight: 16.3 and 10.0).
+template <int FA, typename T>
+__global__ __launch_bounds__(512) void matmul8_few_k(Matmul8Args g) {
+  constexpr int KW = 8, U = 4;
+  __shared__ f32x4 red[KW][64];
+  const int lane = threadIdx.x & 63, l = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int M = g.a.rows, N = g.b.rows, n0 = blockIdx.x * 16, nk = (g.a.k + 127) / 128;
+  const uint32_t ra = min(l, M - 1), rb = min(n0 + l, N - 1);
+  const uint8_t* const pa = g.a.q + ra * g.a.ld + 16 * q;
+  const uint8_t* const pb = g.b.q + rb * g.b.ld + 16 * q;
+  const int sh = 8 * (wave & 3);  // the blocks of a wave have one place in their exponent words
+  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // blocks b0, b0 + KW, ... (UU of them): all loads, then all products
+  auto blocks = [&](auto uu, int b0) {
+    constexpr int UU = decltype(uu)::value;
+    i32x8 fa[UU], fb[UU];
+    uint32_t wa[UU], wb[UU];
 #pragma unroll
-  for (int i = 0; i < SM; ++i) {
-#pragma unroll
-    for (int j = 0; j < SN; ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *(f32x4*)(Ts + l * CS + 32 * j + 8 * q + 4 * h) =
-            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-    asm volatile("" ::: "memory");
-#pragma unroll
-    for (int p = 0; p < 32 / RPP; ++p) {
-      const int r = p * RPP + r_in;
-      float v[8];
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const f32x4 x = *(const f32x4*)(Ts + r * CS + c_in + 4 * q);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e];
-      }
-      const int row = m0 + wm * (BM / 2) + 32 * i + r;
-      if (row < M) store_c<uint16_t, 8>(g, row, n0 + wn * (BN / 2) + c_in, v);
+    for (int u = 0; u < UU; ++u) {
+      const size_t b = b0 + KW * u;
+      fb[u] = __builtin_shufflevector(*(const i32x4*)(pb + b * 128), *(const i32x4*)(pb + b * 128 + 64), 0, 1, 2, 3, 4, 5, 6, 7);
+      wb[u] = (g.b.sc + b / 4 * N)[rb];
+      fa[u] = __builtin_shufflevector(*(const i32x4*)(pa + b * 128), *(const i32x4*)(pa + b * 128 + 64), 0, 1, 2, 3, 4, 5, 6, 7);
+      wa[u] = (g.a.sc + b / 4 * M)[ra];
     }
-    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < UU; ++u) {
+      if constexpr (sizeof(T) == 2) {
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u], fa[u], acc, 0, FA, 0, (int)(wb[u] >> sh), 0,
+                                                               (int)(wa[u] >> sh));
+      } else {
+#pragma unroll
+        for (int w = 0; w < 8; w += 2)
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<E4M3>(fb[u][w], fb[u][w + 1], scale_of((wb[u] >> sh) & 255u)),
+                                                        widen8<FA>(fa[u][w], fa[u][w + 1], scale_of((wa[u] >> sh) & 255u)), acc,
+                                                        0, 0, 0);
+      }
+    }
+  };
+  int b0 = wave;
+  for (; b0 + KW * (U - 1) < nk; b0 += KW * U) blocks(std::integral_constant<int, U>(), b0);
+  for (; b0 < nk; b0 += KW) blocks(std::integral_constant<int, 1>(), b0);
+  red[wave][lane] = acc;
+  __syncthreads();
+  if (wave == 0 && l < M) {
+#pragma unroll
+    for (int w = 1; w < KW; ++w) acc += red[w][lane];
+    float y[4] = {acc[0], acc[1], acc[2], acc[3]};
+    store_c<T, 4>(g, l, n0 + 4 * q, y);
   }
+}
+
+// The splits' sums in their order, bias and old C.
+template <typename T>
+__global__ __launch_bounds__(256) void matmul8_join_k(Matmul8Args g) {
+  const size_t N = g.b.rows, n4 = (N + 3) / 4, all = (size_t)g.a.rows * N;
+  const size_t x = (size_t)blockIdx.x * 256 + threadIdx.x, row = x / n4;
+  const int col = (int)(x % n4) * 4;
+  if (row >= (size_t)g.a.rows) return;
+  const float* p = g.part + row * N + col;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (col + 4 <= (int)N) {
+    for (int i = 0; i < g.splits; ++i, p += all) {
+      const u32x4a u = *(const u32x4a*)p;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += __uint_as_float(u[e]);
+    }
+  } else {
+    for (int i = 0; i < g.splits; ++i, p += all)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (col + e < (int)N) v[e] += p[e];
+  }
+  g.splits = 1;
+  store_c<T, 4>(g, (int)row, col, v);
+}
+
+template <int FA, int BM, int BN>
+static void launch_quad(const Matmul8Args& g, hipStream_t s) {
+  const dim3 grid((unsigned)((g.a.rows + BM - 1) / BM) * (unsigned)((g.b.rows + BN - 1) / BN), g.splits);
+  hipLaunchKernelGGL((matmul8_quad_k<FA, BM, BN, 6, 5>), grid, dim3(256), 0, s, g);
 }
 
 template <int FA, typename T, int BM, int BN, int WM, int WN, int KG>
 static void launch_tile(const Matmul8Args& g, hipStream_t s) {
-  const dim3 grid((unsigned)((g.a.rows + BM - 1) / BM) * (unsigned)((g.b.rows + BN - 1) / BN));
+  const dim3 grid((unsigned)((g.a.rows + BM - 1) / BM) * (unsigned)((g.b.rows + BN - 1) / BN), g.splits);
   hipLaunchKernelGGL((matmul8_tile_k<FA, T, BM, BN, WM, WN, KG>), grid, dim3(64 * WM * WN * KG), 0, s, g);
+}
+
+// ---------------------------------------------------------------------- launch
+enum Kind8 { K8_FEW, K8_64, K8_128, K8_256 };
+
+// Tiles and splits of k: the least estimated time (us) = rounds of the 256 CUs x (blocks
+// of 128 of a split x time per block + prologue and epilogue), and for a split the
+// second launch and the sums' way through memory.  The times per block are those
+// measured with every CU busy: bf16 0.25 (64 x 64), 0.58 (128 x 128; 1.0 for two on a
+// CU), 1.4 (256 x 256); fp32 0.29, 0.78 (1.65), 3.2.  Over 110 sizes drawn from 17 .. 9216
+// rows, 64 .. 16384 columns and k the choice takes 1.00 times the best of three
+// tiles x eight splits in the mean and 1.17 times at most.  Examples (us; 64 x 64 in one
+// and four splits, 128 x 128 in one and eight, bf16): 37 x 4096, k 12288: 34, 16, 59, 17;
+// 128 rows: 34, 27, 63, 22; 1024 x 1024, k 4096: 12, 22, 18, -; 1024 x 4096, k 4096: 37, 64,
+// 20, -.  The single-token kernel up to 16 rows: 13.8 at 16 x 4096, k 12288 (64 x 64 tiles in
+// four splits: 15.0).
+
+size_t matmul8_plan(Matmul8Args& g) {
+  const int M = g.a.rows, N = g.b.rows, nb = (g.a.k + 127) / 128;
+  g.kind = K8_FEW;
+  g.splits = 1;
+  g.per_split = nb;
+  if (M <= 16) return 0;
+  const bool f32 = g.out_dt == F32;
+  double bt = 1e300;
+  for (int kind = K8_64; kind <= K8_256; ++kind) {
+    const int b = kind == K8_64 ? 64 : kind == K8_128 ? 128 : 256;
+    const long tiles = (long)((M + b - 1) / b) * ((N + b - 1) / b);
+    for (int s = 1; s <= 16; ++s) {
+      const int ps = s == 1 ? nb : ((nb + s - 1) / s + 3) / 4 * 4;
+      const long wgs = tiles * s;
+      if (s > 1 && (ps < 8 || wgs > 1024)) break;  // more only costs more
+      if ((nb + ps - 1) / ps != s) continue;
+      double t;
+      if (kind == K8_64) {
+        t = 2.0 + (wgs + 255) / 256 * (ps * (f32 ? 0.29 : 0.25) + 1.5);
+      } else if (kind == K8_128) {  // two workgroups per CU
+        const double one = ps * (f32 ? 0.78 : 0.58) + 2.5, two = ps * (f32 ? 1.65 : 1.0) + 3.5;
+        const long rest = wgs % 512;
+        t = 2.0 + wgs / 512 * two + (rest == 0 ? 0.0 : rest <= 256 ? one : two);
+      } else {
+        t = 4.0 + (wgs + 255) / 256 * (ps * (f32 ? 3.2 : 1.4) + 8.5);
+      }
+      if (s > 1) t += 4.0 + (double)M * N * s * 8 / 4.5e6;
+      if (t < bt) {
+        bt = t;
+        g.kind = kind;
+        g.splits = s;
+        g.per_split = ps;
+      }
+    }
+  }
+  return g.splits > 1 ? (size_t)g.splits * M * N * sizeof(float) : 0;
 }
 
 template <int FA, typename T>
 static void launch_matmul8(const Matmul8Args& g, hipStream_t s) {
-  const long t256 = (long)((g.a.rows + 255) / 256) * ((g.b.rows + 255) / 256);
-  const long t128 = (long)((g.a.rows + 127) / 128) * ((g.b.rows + 127) / 128);
-  if (t256 >= 128) {
-    if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((matmul8_quad_k<FA, 256, 256, 6, 5>), dim3((unsigned)t256), dim3(256), 0, s, g);
+  if (g.kind == K8_FEW) {
+    hipLaunchKernelGGL((matmul8_few_k<FA, T>), dim3((g.b.rows + 15) / 16), dim3(512), 0, s, g);
+    return;
+  }
+  if (g.kind == K8_64) return launch_tile<FA, T, 64, 64, 1, 2, 2>(g, s);
+  if constexpr (sizeof(T) == 2) {
+    if (g.kind == K8_128) launch_quad<FA, 128, 128>(g, s);
+    else launch_quad<FA, 256, 256>(g, s);
+  } else {
+    if (g.kind == K8_128) launch_tile<FA, T, 128, 128, 2, 2, 1>(g, s);
     else launch_tile<FA, T, 256, 256, 2, 4, 1>(g, s);
   }
-  else if (t128 >= 128) launch_tile<FA, T, 128, 128, 2, 2, 1>(g, s);
-  else launch_tile<FA, T, 64, 64, 1, 2, 4>(g, s);
 }
 
 int matmul8(const Matmul8Args& g, hipStream_t s) {
@@ -649,6 +876,13 @@ int matmul8(const Matmul8Args& g, hipStream_t s) {
     else launch_matmul8<E4M3, float>(g, s);
   }
   JG_CHECK_LAUNCH("matmul8");
+  if (g.splits > 1) {
+    const size_t n = (size_t)g.a.rows * ((g.b.rows + 3) / 4);
+    const dim3 grid((unsigned)((n + 255) / 256));
+    if (g.out_dt == BF16) hipLaunchKernelGGL(matmul8_join_k<uint16_t>, grid, dim3(256), 0, s, g);
+    else hipLaunchKernelGGL(matmul8_join_k<float>, grid, dim3(256), 0, s, g);
+    JG_CHECK_LAUNCH("matmul8_join");
+  }
   return 0;
 }
 

@@ -66,7 +66,12 @@ struct Matmul8Args {
   const void* bias;  // out_dt, or nullptr
   void* out; size_t ldo; int out_dt;
   float beta;        // 0 or 1
+  // a long k over few tiles is split: sums of each split, added by a second launch
+  float* part;
+  int kind, splits, per_split;  // set by matmul8_plan
 };
+// Chooses the tiles and splits (from the sizes and out_dt); returns the bytes of `part`.
+size_t matmul8_plan(Matmul8Args& a);
 int matmul8(const Matmul8Args& a, hipStream_t s);
 
 struct GradSeg {

@@ -189,6 +189,28 @@ def test_matmul8_exact_on_whole_numbers(ctx, m, n, k, dt):
     assert torch.equal(wide[:, 1:n + 1].cpu(), (exact + bias.double().cpu()).to(dt))
 
 
+@pytest.mark.parametrize("m,n,k", [(17, 131, 9000), (40, 515, 12288), (129, 257, 8001), (640, 300, 7000), (1100, 70, 15000)])
+@pytest.mark.parametrize("dt", [BF, FP])
+def test_matmul8_with_a_split_contraction(m, n, k, dt):
+    """Few tiles and a long k: sums of each split, joined in order; the workspace holds
+    NaN before."""
+    say(f"case: matmul8 split {m}x{n}x{k} {dt}")
+    ctx = pk.Context(pk.config("tiny"))
+    a, va = whole_mat(m, m, k, "e5m2", 1)
+    b, vb = whole_mat(n + 1, n, k, "e4m3", 1)
+    out = torch.full((m, n + 2), 3.0, dtype=dt, device="cuda")
+    bias = torch.arange(n, dtype=FP).remainder(7).to(dt).cuda()
+    ctx.matmul8(a, b, out[:, 1:n + 1])
+    ctx._ws.view(torch.uint8).fill_(0xFF)
+    ctx.matmul8(a, b, out[:, 1:n + 1], bias=bias)
+    want = torch.from_numpy(va @ vb.T) + bias.double().cpu()
+    assert torch.equal(out[:, 1:n + 1].cpu(), want.to(dt))
+    out[:, 1:n + 1] = 2.0
+    ctx.matmul8(a, b, out[:, 1:n + 1], bias=bias, beta=1.0)
+    assert torch.equal(out[:, 1:n + 1].cpu(), (want + 2).to(dt))
+    assert bool((out[:, 0] == 3).all()) and bool((out[:, n + 1] == 3).all())
+
+
 @pytest.mark.parametrize("m,n,k,fmt", [(1, 300, 3000, "e4m3"), (5, 129, 8200, "e5m2"), (40, 200, 2000, "e4m3"),
                                        (200, 333, 2500, "e5m2"), (600, 700, 1100, "e4m3")])
 def test_matmul8_on_quantised_values(ctx, m, n, k, fmt):

@@ -87,6 +87,26 @@ def test_matmul8_refuses_bad_arguments(ctx):
     assert b"E4M3" in L.jagg_last_error()
 
 
+def test_matmul8_workspace(ctx):
+    """A long contraction over a small result needs one, few rows and large results none."""
+    L, h = ctx
+    n = ctypes.c_size_t()
+
+    def need(*a):
+        assert L.jagg_matmul8_bytes(*a, ctypes.byref(n)) == 0
+        return n.value
+
+    assert need(37, 4096, 12288, 1) >= 2 * 37 * 4096 * 4 and need(512, 512, 9216, 0) >= 2 * 512 * 512 * 4
+    assert need(1, 4096, 12288, 1) == need(16, 4096, 12288, 0) == need(9216, 16384, 4096, 1) == need(100, 100, 100, 1) == 0
+    bytes_ = need(37, 4096, 12288, 1)
+    args = (m8(37, 12288), m8(4096, 12288), None, P, 4096, 1, 0.0)
+    assert L.jagg_matmul8(h, *args) == 1 and b"jagg_matmul8_bytes" in L.jagg_last_error()
+    assert L.jagg_ctx_set_workspace(h, P, bytes_ - 1) == 0
+    assert L.jagg_matmul8(h, *args) == 1 and b"jagg_matmul8_bytes" in L.jagg_last_error()
+    assert L.jagg_matmul8_bytes(0, 1, 1, 0, ctypes.byref(n)) == 1 and L.jagg_matmul8_bytes(1, 1, 1, 2, ctypes.byref(n)) == 1
+    assert L.jagg_matmul8_bytes(1, 1, 1, 0, None) == 1
+
+
 NORM = dict(x=P, ldx=256, r=None, ldr=0, gain=P, rows=8, cols=256, dt=1, eps=1e-6, h=None, ldh=0, y=m8(8, 256), rstd=P)
 
 
