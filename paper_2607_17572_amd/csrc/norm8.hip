@@ -9,7 +9,10 @@
 // hold NV vectors of 8 columns each, vector i of thread t at column 8 (i NT + t); 16
 // neighbouring lanes then hold one block of 128 columns and a wave one exponent
 // word.  Both are bound by memory: every tensor is read or written once.
+#include <algorithm>
+
 #include "q8.h"
+#include "tile.h"
 
 namespace jg {
 
@@ -115,71 +118,197 @@ int rmsnorm8(const Norm8Args& a, hipStream_t s) {
 }
 
 // ------------------------------------------------------------------ backward
-// Each of `workers` thread rows takes rows w, w + workers, ... and keeps its sums of
-// dgain in registers; they go to part[worker][cols] and are added in that order.
-static int norm8_threads(int cols) { return cols <= 2048 ? 64 : cols <= 8192 ? 256 : 1024; }
-static int norm8_workers(int rows, int cols) {
-  const int per = norm8_threads(cols) == 64 ? 4 : 1;
-  const int blocks = 512, want = (rows + per - 1) / per;
-  return (want < blocks ? want : blocks) * per;
+// A workgroup takes rows w, w + workgroups, ... (with NT = 64 each of its four waves does) and
+// keeps its sums of dgain in registers; they go to part[workgroup][cols] and are
+// added in that order.  A row's loads are issued together and stay in their storage type
+// until they are used: at 4096 columns in bf16 a wave holds a row in 96 registers, so that
+// eight rows of 24 KB are on their way in a CU.
+static int norm8_threads(int cols, int dt) {
+  return cols <= (dt == BF16 ? 4096 : 2048) ? 64 : cols <= 8192 ? 256 : 1024;
 }
-size_t rmsnorm8_grad_bytes(int rows, int cols) { return (size_t)norm8_workers(rows, cols) * cols * sizeof(float); }
+static int norm8_workgroups(int rows, int cols, int dt) {
+  const int per = norm8_threads(cols, dt) == 64 ? 4 : 1, want = (rows + per - 1) / per;
+  return want < 512 ? want : 512;
+}
+size_t rmsnorm8_grad_bytes(int rows, int cols) {
+  const size_t w = std::max(norm8_workgroups(rows, cols, BF16), norm8_workgroups(rows, cols, F32));
+  return w * cols * sizeof(float);
+}
 
-template <typename T, int NT, int NV>
+// 16 bytes of a buffer; none (zeros) past its end
+__device__ __forceinline__ u32x4a buf_load16(__amdgpu_buffer_rsrc_t r, int off) {
+  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+}
+__device__ __forceinline__ void buf_store16(u32x4a v, __amdgpu_buffer_rsrc_t r, int off) {
+  __builtin_amdgcn_raw_buffer_store_b128(v, r, off, 0, 0);
+}
+
+// A row of a matrix (p == nullptr: zeros).  V8: its elements are a multiple of eight at a
+// multiple of 16 bytes; vectors then are whole or past the end, where a buffer's
+// range check gives zeros and stores nothing, without a branch.
+template <typename T, bool V8>
+struct Row8 {
+  T* p;
+  int cols;
+  __device__ __forceinline__ Row8(const void* m, size_t ld, int row, int n) {
+    p = m ? (T*)m + (size_t)row * ld : nullptr;
+    cols = m ? n : 0;
+  }
+};
+
+// eight elements of a row as stored
+template <typename T, bool V8>
+struct Raw8 {
+  u32x4a r[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const Row8<T, V8>& row, int c) {
+    if constexpr (V8) {
+      const __amdgpu_buffer_rsrc_t b = make_rsrc(row.p, (long)row.cols * sizeof(T));
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) r[i] = buf_load16(b, c * (int)sizeof(T) + 16 * i);
+    } else {
+      float v[8];
+      load8(row.p, c, row.cols, v);
+      set(v);
+    }
+  }
+  __device__ __forceinline__ void store(const Row8<T, V8>& row, int c) const {
+    if constexpr (V8) {
+      const __amdgpu_buffer_rsrc_t b = make_rsrc(row.p, (long)row.cols * sizeof(T));
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) buf_store16(r[i], b, c * (int)sizeof(T) + 16 * i);
+    } else {
+      float v[8];
+      get(v);
+      store8(row.p, c, row.cols, v);
+    }
+  }
+  __device__ __forceinline__ void set(const float* v) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if constexpr (sizeof(T) == 2) {
+        r[0][w] = (uint32_t)f2bf(v[2 * w]) | (uint32_t)f2bf(v[2 * w + 1]) << 16;
+      } else {
+        r[0][w] = __float_as_uint(v[w]);
+        r[1][w] = __float_as_uint(v[4 + w]);
+      }
+    }
+  }
+  // forgets what is known of the values: a later get() unpacks again, and the fp32
+  // values need not be kept
+  __device__ __forceinline__ void renew() {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) asm("" : "+v"(r[i]));
+  }
+  __device__ __forceinline__ void get(float* v) const {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if constexpr (sizeof(T) == 2) {
+        v[2 * w] = bf2f(r[0][w] & 0xffffu);
+        v[2 * w + 1] = bf2f(r[0][w] >> 16);
+      } else {
+        v[w] = __uint_as_float(r[0][w]);
+        v[4 + w] = __uint_as_float(r[1][w]);
+      }
+    }
+  }
+};
+
+template <typename T, int NT, int NV, bool V8>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm8_grad_k(Norm8Grad a) {
   constexpr int RPB = NT < 256 ? 256 / NT : 1;
+  constexpr bool WAVE = NT == 64;
   __shared__ float sh[16];
-  const int t = threadIdx.x % NT, worker = blockIdx.x * RPB + threadIdx.x / NT, workers = gridDim.x * RPB;
-  float g[NV][8], dg[NV][8];
+  __shared__ __attribute__((aligned(16))) float sum[WAVE ? 512 * NV : 1];
+  __shared__ __attribute__((aligned(16))) T gain[WAVE ? 512 * NV : 1];  // as the lanes hold it
+  const int t = threadIdx.x % NT, sub = WAVE ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0, workers = gridDim.x * RPB;
+  Raw8<T, V8> g[WAVE ? 1 : NV];
+  float dg[NV][8];
+  if constexpr (WAVE) {
+    for (int i = threadIdx.x; i < 512 * NV; i += 256) gain[i] = i < a.cols ? ((const T*)a.gain)[i] : (T)0;
+    __syncthreads();
+  } else {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    load8((const T*)a.gain, 8 * (i * NT + t), a.cols, g[i]);
+    for (int i = 0; i < NV; ++i) g[i].load(Row8<T, V8>(a.gain, 0, 0, a.cols), 8 * (i * NT + t));
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) dg[i][e] = 0.f;
-  }
   const float inv_c = 1.f / (float)a.cols;
-  for (int row = worker; row < a.rows; row += workers) {
-    const T* dyp = (const T*)a.dy + (size_t)row * a.lddy;
-    const T* hp = (const T*)a.h + (size_t)row * a.ldh;
+  for (int row = blockIdx.x * RPB + sub; row < a.rows; row += workers) {
+    Raw8<T, V8> dy[NV], h[NV], dh[NV];
+    const Row8<T, V8> rdy(a.dy, a.lddy, row, a.cols), rh(a.h, a.ldh, row, a.cols), rdh(a.dh, a.lddh, row, a.cols),
+        rdx(a.dx, a.lddx, row, a.cols);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) dy[i].load(rdy, 8 * (i * NT + t));
+#pragma unroll
+    for (int i = 0; i < NV; ++i) h[i].load(rh, 8 * (i * NT + t));
+#pragma unroll
+    for (int i = 0; i < NV; ++i) dh[i].load(rdh, 8 * (i * NT + t));
     const float rs = a.rstd[row];
-    float dy[NV][8], h[NV][8], dot = 0.f;
+    auto up_of = [&](int i, float* up, float* n, float* d) {  // a = dy gain, n = h rstd, dy
+      float gv[8];
+      if constexpr (WAVE) load8(gain + 8 * (i * 64 + t), gv);
+      else g[i].get(gv);
+      dy[i].get(d);
+      h[i].get(n);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        n[e] *= rs;
+        up[e] = d[e] * gv[e];
+      }
+    };
+    float dot = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      load8(dyp, 8 * (i * NT + t), a.cols, dy[i]);
-      load8(hp, 8 * (i * NT + t), a.cols, h[i]);
+      float up[8], n[8], d[8];
+      up_of(i, up, n, d);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        dg[i][e] = fmaf(d[e], n[e], dg[i][e]);
+        dot = fmaf(up[e], n[e], dot);
+      }
+    }
+    dot = row_sum<NT>(dot, sh) * inv_c;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      dy[i].renew();
+      h[i].renew();
     }
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float n = h[i][e] * rs, up = dy[i][e] * g[i][e];
-        dg[i][e] = fmaf(dy[i][e], n, dg[i][e]);
-        h[i][e] = n;
-        dy[i][e] = up;
-        dot = fmaf(up, n, dot);
-      }
-    dot = row_sum<NT>(dot, sh) * inv_c;
-    T* dxp = (T*)a.dx + (size_t)row * a.lddx;
-    const T* dhp = (const T*)a.dh + (size_t)row * a.lddh;
-#pragma unroll
     for (int i = 0; i < NV; ++i) {
-      float o[8];
-      if (a.dh) load8(dhp, 8 * (i * NT + t), a.cols, o);
+      float up[8], n[8], d[8], o[8];
+      up_of(i, up, n, d);
+      dh[i].get(o);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float d = rs * (dy[i][e] - h[i][e] * dot);
-        o[e] = a.dh ? o[e] + d : d;
-      }
-      store8(dxp, 8 * (i * NT + t), a.cols, o);
+      for (int e = 0; e < 8; ++e) o[e] += rs * (up[e] - n[e] * dot);
+      dh[i].set(o);
+      dh[i].store(rdx, 8 * (i * NT + t));
     }
   }
-  float* p = a.part + (size_t)worker * a.cols;
+  float* p = a.part + (size_t)blockIdx.x * a.cols;
+  if constexpr (WAVE) {  // the waves' sums, in wave order
+    for (int w = 0; w < RPB; ++w) {
+      __syncthreads();
+      if (sub != w) continue;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) store8(p, 8 * (i * NT + t), a.cols, dg[i]);
+      for (int i = 0; i < NV; ++i) {
+        float* const q = sum + 8 * (i * 64 + t);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[e] = w ? q[e] + dg[i][e] : dg[i][e];
+      }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.cols; i += 256) p[i] = sum[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) store8(p, 8 * (i * NT + t), a.cols, dg[i]);
+  }
 }
 
-// dgain = beta dgain + sum of part over the workers: 64 columns per workgroup, its 16
-// waves take every 16th worker.
+// dgain = beta dgain + sum of part over the workgroups: 64 columns per workgroup, its 16
+// waves take every 16th row of part.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm8_dgain_k(const float* part, int workers, int cols, T* dgain, float beta) {
   __shared__ float sh[16][64];
@@ -200,17 +329,21 @@ __global__ __launch_bounds__(1024) void norm8_dgain_k(const float* part, int wor
 template <typename T, int NT, int NV>
 struct Norm8G {
   static void go(const Norm8Grad& a, hipStream_t s) {
-    constexpr int RPB = NT < 256 ? 256 / NT : 1;
-    const int workers = norm8_workers(a.rows, a.cols);
-    hipLaunchKernelGGL((rmsnorm8_grad_k<T, NT, NV>), dim3(workers / RPB), dim3(NT < 256 ? 256 : NT), 0, s, a);
+    const dim3 grid(norm8_workgroups(a.rows, a.cols, a.dt)), block(NT < 256 ? 256 : NT);
+    const size_t es = dsize(a.dt);
+    const bool v8 = a.cols % 8 == 0 && (a.lddy * es | a.ldh * es | a.lddh * es | a.lddx * es) % 16 == 0 &&
+                    ((uintptr_t)a.dy | (uintptr_t)a.h | (uintptr_t)a.dh | (uintptr_t)a.dx | (uintptr_t)a.gain) % 16 == 0;
+    if (v8) hipLaunchKernelGGL((rmsnorm8_grad_k<T, NT, NV, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((rmsnorm8_grad_k<T, NT, NV, false>), grid, block, 0, s, a);
   }
 };
 
 int rmsnorm8_grad(const Norm8Grad& a, hipStream_t s) {
-  if (a.dt == BF16) by_width<Norm8G, uint16_t>(a, s);
+  if (a.dt == BF16 && a.cols > 2048 && a.cols <= 4096) Norm8G<uint16_t, 64, 8>::go(a, s);
+  else if (a.dt == BF16) by_width<Norm8G, uint16_t>(a, s);
   else by_width<Norm8G, float>(a, s);
   JG_CHECK_LAUNCH("rmsnorm8_grad");
-  const int workers = norm8_workers(a.rows, a.cols);
+  const int workers = norm8_workgroups(a.rows, a.cols, a.dt);
   const dim3 grid((a.cols + 63) / 64);
   if (a.dgain_dt == BF16)
     hipLaunchKernelGGL(norm8_dgain_k<uint16_t>, grid, dim3(1024), 0, s, a.part, workers, a.cols, (uint16_t*)a.dgain, a.beta);
