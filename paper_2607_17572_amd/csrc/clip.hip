@@ -17,7 +17,10 @@
 
 namespace jg {
 
-constexpr int GS = 112, CH = 8192;
+// Elements of a chunk: 32 a thread, or 8 where the list then still has no more chunks
+// than the card's CUs take at once (a small gradient: 0.3 million elements, 48 tensors).
+constexpr int GS = 112, CH = 8192, CH_SMALL = 2048;
+constexpr size_t SMALL = 1u << 21;
 
 struct GradSegs {
   const void* src[GS];
@@ -26,7 +29,7 @@ struct GradSegs {
   unsigned first[GS];    // chunk at which a piece begins
   unsigned char dt[GS];  // src type | dst type << 1
   int count;
-  unsigned chunks;
+  unsigned chunks, ch;
 };
 static_assert(sizeof(GradSegs) <= 3400, "kernel arguments");
 
@@ -57,12 +60,15 @@ __device__ __forceinline__ double merge(bool max, double a, double b) {
 template <typename T, bool MAX>
 __device__ __forceinline__ void norm_chunk(const T* p, unsigned n, double& acc, uint32_t& top) {
   unsigned i = threadIdx.x * 8;
-  for (; i + 8 <= n; i += 256 * 8) {
-    float v[8];
-    load8(p + i, v);
-    take<MAX>(acc, top, v);
+  if (n == CH) {  // four vectors in flight
+    float v[4][8];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) load8(p + i + u * 2048, v[u]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) take<MAX>(acc, top, v[u]);
+    return;
   }
-  if (i < n) {
+  for (; i < n; i += 2048) {
     float v[8];
     load8(p, (int)i, (int)n, v);
     take<MAX>(acc, top, v);
@@ -76,8 +82,8 @@ __global__ __launch_bounds__(256) void grad_norm_k(GradSegs g, double* part, int
   uint32_t top = 0;
   for (unsigned c = blockIdx.x; c < g.chunks; c += gridDim.x) {
     const int s = piece_of(g, c);
-    const size_t at = (size_t)(c - g.first[s]) * CH, left = g.n[s] - at;
-    const unsigned n = left < CH ? (unsigned)left : CH;
+    const size_t at = (size_t)(c - g.first[s]) * g.ch, left = g.n[s] - at;
+    const unsigned n = left < g.ch ? (unsigned)left : g.ch;
     if (g.dt[s] & 1) norm_chunk<uint16_t, MAX>((const uint16_t*)g.src[s] + at, n, acc, top);
     else norm_chunk<float, MAX>((const float*)g.src[s] + at, n, acc, top);
   }
@@ -112,7 +118,20 @@ __global__ __launch_bounds__(256) void grad_norm_out_k(const double* part, int n
 
 template <typename T, typename D>
 __device__ __forceinline__ void scale_chunk(const T* p, D* d, unsigned n, float c) {
-  for (unsigned i = threadIdx.x * 8; i < n; i += 256 * 8) {
+  unsigned i = threadIdx.x * 8;
+  if (n == CH) {
+    float v[4][8];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) load8(p + i + u * 2048, v[u]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[u][e] *= c;
+      store8(d + i + u * 2048, v[u]);
+    }
+    return;
+  }
+  for (; i < n; i += 2048) {
     float v[8];
     load8(p, (int)i, (int)n, v);
 #pragma unroll
@@ -134,8 +153,8 @@ __global__ __launch_bounds__(256) void grad_scale_k(GradSegs g, const double* pa
   for (unsigned k = blockIdx.x; k < g.chunks; k += gridDim.x) {
     const int s = piece_of(g, k);
     if (!clip && g.src[s] == g.dst[s]) continue;
-    const size_t at = (size_t)(k - g.first[s]) * CH, left = g.n[s] - at;
-    const unsigned n = left < CH ? (unsigned)left : CH;
+    const size_t at = (size_t)(k - g.first[s]) * g.ch, left = g.n[s] - at;
+    const unsigned n = left < g.ch ? (unsigned)left : g.ch;
     const int t = g.dt[s];
     if (t == 3) scale_chunk((const uint16_t*)g.src[s] + at, (uint16_t*)g.dst[s] + at, n, cf);
     else if (t == 1) scale_chunk((const uint16_t*)g.src[s] + at, (float*)g.dst[s] + at, n, cf);
@@ -146,8 +165,9 @@ __global__ __launch_bounds__(256) void grad_scale_k(GradSegs g, const double* pa
 
 // Calls f(pieces) for each launch's worth of the list, empty tensors left out.
 template <class F>
-static int for_pieces(GradAt at, const void* list, int count, F f) {
+static int for_pieces(GradAt at, const void* list, int count, int ch, F f) {
   GradSegs g;
+  g.ch = ch;
   g.count = 0;
   g.chunks = 0;
   GradSeg cur{};
@@ -160,10 +180,10 @@ static int for_pieces(GradAt at, const void* list, int count, F f) {
   };
   auto put = [&](const GradSeg& s) -> int {
     // a launch's chunk numbers fit 31 bits: a longer piece is cut
-    const size_t most = (size_t)CH << 28;
+    const size_t most = (size_t)ch << 28;
     for (size_t done = 0; done < s.n;) {
       const size_t n = std::min(s.n - done, most);
-      const unsigned chunks = (unsigned)((n + CH - 1) / CH);
+      const unsigned chunks = (unsigned)((n + ch - 1) / ch);
       if (g.count == GS || g.chunks > (1u << 28))
         if (int rc = flush()) return rc;
       const int i = g.count++;
@@ -196,13 +216,19 @@ static int for_pieces(GradAt at, const void* list, int count, F f) {
   return flush();
 }
 
+static int chunk_of(GradAt at, const void* list, int count) {
+  size_t n = 0;
+  for (int i = 0; i < count; ++i) n += at(list, i).n;
+  return n <= SMALL ? CH_SMALL : CH;
+}
+
 // Partials of the norm of the whole list; returns their number (0: no elements), -1 on an error.
-static int norm_pass(GradAt at, const void* list, int count, bool largest, double* part, hipStream_t s) {
+static int norm_pass(GradAt at, const void* list, int count, int ch, bool largest, double* part, hipStream_t s) {
   size_t chunks = 0;  // of the whole list: every launch has workgroups for the longest
-  for (int i = 0; i < count; ++i) chunks += (at(list, i).n + CH - 1) / CH;
+  for (int i = 0; i < count; ++i) chunks += (at(list, i).n + ch - 1) / ch;
   const int nparts = (int)std::min<size_t>(chunks, GRAD_PART);
   bool carry = false;
-  const int rc = for_pieces(at, list, count, [&](const GradSegs& g) -> int {
+  const int rc = for_pieces(at, list, count, ch, [&](const GradSegs& g) -> int {
     if (largest) hipLaunchKernelGGL(grad_norm_k<true>, dim3(nparts), dim3(256), 0, s, g, part, carry ? 1 : 0);
     else hipLaunchKernelGGL(grad_norm_k<false>, dim3(nparts), dim3(256), 0, s, g, part, carry ? 1 : 0);
     JG_CHECK_LAUNCH("grad_norm");
@@ -213,7 +239,7 @@ static int norm_pass(GradAt at, const void* list, int count, bool largest, doubl
 }
 
 int grad_norm(GradAt at, const void* list, int count, bool largest, double* part, double* out, hipStream_t s) {
-  const int nparts = norm_pass(at, list, count, largest, part, s);
+  const int ch = chunk_of(at, list, count), nparts = norm_pass(at, list, count, ch, largest, part, s);
   if (nparts < 0) return 3;
   if (largest) hipLaunchKernelGGL(grad_norm_out_k<true>, dim3(1), dim3(256), 0, s, part, nparts, out);
   else hipLaunchKernelGGL(grad_norm_out_k<false>, dim3(1), dim3(256), 0, s, part, nparts, out);
@@ -223,7 +249,7 @@ int grad_norm(GradAt at, const void* list, int count, bool largest, double* part
 
 int grad_clip(GradAt at, const void* list, int count, bool largest, double max_norm, double* part, double* out,
               hipStream_t s) {
-  const int nparts = norm_pass(at, list, count, largest, part, s);
+  const int ch = chunk_of(at, list, count), nparts = norm_pass(at, list, count, ch, largest, part, s);
   if (nparts < 0) return 3;
   auto scale = [&](const GradSegs& g) -> int {
     const unsigned grid = std::max(1u, std::min<unsigned>(g.chunks, 2048));
@@ -236,9 +262,10 @@ int grad_clip(GradAt at, const void* list, int count, bool largest, double max_n
     GradSegs none;
     none.count = 0;
     none.chunks = 0;
+    none.ch = ch;
     return scale(none);
   }
-  return for_pieces(at, list, count, scale);
+  return for_pieces(at, list, count, ch, scale);
 }
 
 }  // namespace jg
