@@ -203,9 +203,15 @@ def _ptrs(tensors):
     return (ctypes.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
 
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 # -------------------------------------------------- arguments of the operators
@@ -215,24 +221,28 @@ def _refuse(msg: str):
 
 def _dtype_of(t, name: str) -> int:
     torch = _torch()
-    if t.dtype is torch.bfloat16:
+    dt = t.dtype
+    if dt is torch.bfloat16:
         return BF16
-    if t.dtype is torch.float32:
+    if dt is torch.float32:
         return F32
     _refuse(f"{name} must be bf16 or fp32")
 
 
 def _vec(t, name: str, n: int, dtype, device):
     """Pointer of a contiguous vector of n elements."""
-    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1) or t.device != device:
+    if t.dtype is not dtype or t.dim() != 1 or t.numel() != n or not t.is_contiguous() or t.device != device:
         _refuse(f"{name} must be a contiguous vector of {n} elements of {dtype} on {device}")
     return t.data_ptr()
 
 
 def _rows(t, name: str, rows: int, cols: int, dtype, device):
     """(pointer, row stride) of a matrix whose rows are contiguous."""
-    if t.dtype is not dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.device != device:
+    sh = t.shape
+    if t.dtype is not dtype or len(sh) != 2 or sh[0] != rows or sh[1] != cols or t.device != device:
         _refuse(f"{name} must be {rows} x {cols} of {dtype} on {device}")
+    if t.is_contiguous():
+        return t.data_ptr(), cols
     st = t.stride()
     if (cols > 1 and st[1] != 1) or (rows > 1 and st[0] < cols):
         _refuse(f"{name} must have contiguous rows that do not overlap")

@@ -17,30 +17,36 @@
 
 namespace jg {
 
-// Elements of a chunk: 32 a thread, or 8 where the list then still has no more chunks
+// Elements of a chunk: 64 a thread, or 8 where the list then still has no more chunks
 // than the card's CUs take at once (a small gradient: 0.3 million elements, 48 tensors).
-constexpr int GS = 112, CH = 8192, CH_SMALL = 2048;
+constexpr int GS = 112, CH = 16384, CH_SMALL = 2048;
 constexpr size_t SMALL = 1u << 21;
 
 struct GradSegs {
   const void* src[GS];
   void* dst[GS];
   size_t n[GS];
-  unsigned first[GS];    // chunk at which a piece begins
+  unsigned first[GS];  // chunk at which a piece begins
   unsigned char dt[GS];  // src type | dst type << 1
   int count;
   unsigned chunks, ch;
 };
 static_assert(sizeof(GradSegs) <= 3400, "kernel arguments");
 
-__device__ __forceinline__ int piece_of(const GradSegs& g, unsigned c) {
-  int lo = 0, hi = g.count - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (g.first[mid] <= c) lo = mid; else hi = mid - 1;
+// The piece of a chunk: the pieces' first chunks lie in the lanes, two each, so that
+// finding one reads no memory.
+static_assert(GS <= 128, "two pieces per lane");
+struct Pieces {
+  unsigned f0, f1;
+  __device__ __forceinline__ explicit Pieces(const GradSegs& g) {
+    const int lane = threadIdx.x & 63;
+    f0 = lane < g.count ? g.first[lane] : ~0u;
+    f1 = lane + 64 < g.count ? g.first[lane + 64] : ~0u;
   }
-  return lo;
-}
+  __device__ __forceinline__ int of(unsigned c) const {
+    return __popcll(__ballot(f0 <= c)) + __popcll(__ballot(f1 <= c)) - 1;
+  }
+};
 
 template <bool MAX>
 __device__ __forceinline__ void take(double& acc, uint32_t& top, const float* v) {
@@ -60,12 +66,12 @@ __device__ __forceinline__ double merge(bool max, double a, double b) {
 template <typename T, bool MAX>
 __device__ __forceinline__ void norm_chunk(const T* p, unsigned n, double& acc, uint32_t& top) {
   unsigned i = threadIdx.x * 8;
-  if (n == CH) {  // four vectors in flight
-    float v[4][8];
+  if (n == CH) {  // eight vectors in flight
+    float v[8][8];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) load8(p + i + u * 2048, v[u]);
+    for (int u = 0; u < 8; ++u) load8(p + i + u * 2048, v[u]);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) take<MAX>(acc, top, v[u]);
+    for (int u = 0; u < 8; ++u) take<MAX>(acc, top, v[u]);
     return;
   }
   for (; i < n; i += 2048) {
@@ -80,8 +86,9 @@ __global__ __launch_bounds__(256) void grad_norm_k(GradSegs g, double* part, int
   __shared__ double sh[4];
   double acc = 0.0;
   uint32_t top = 0;
+  const Pieces pieces(g);
   for (unsigned c = blockIdx.x; c < g.chunks; c += gridDim.x) {
-    const int s = piece_of(g, c);
+    const int s = pieces.of(c);
     const size_t at = (size_t)(c - g.first[s]) * g.ch, left = g.n[s] - at;
     const unsigned n = left < g.ch ? (unsigned)left : g.ch;
     if (g.dt[s] & 1) norm_chunk<uint16_t, MAX>((const uint16_t*)g.src[s] + at, n, acc, top);
@@ -120,11 +127,11 @@ template <typename T, typename D>
 __device__ __forceinline__ void scale_chunk(const T* p, D* d, unsigned n, float c) {
   unsigned i = threadIdx.x * 8;
   if (n == CH) {
-    float v[4][8];
+    float v[8][8];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) load8(p + i + u * 2048, v[u]);
+    for (int u = 0; u < 8; ++u) load8(p + i + u * 2048, v[u]);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < 8; ++u) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[u][e] *= c;
       store8(d + i + u * 2048, v[u]);
@@ -150,8 +157,9 @@ __global__ __launch_bounds__(256) void grad_scale_k(GradSegs g, const double* pa
   const double c = clip ? max_norm / norm : 1.0;
   if (out && blockIdx.x == 0 && threadIdx.x == 0) { out[0] = norm; out[1] = c; }
   const float cf = (float)c;
+  const Pieces pieces(g);
   for (unsigned k = blockIdx.x; k < g.chunks; k += gridDim.x) {
-    const int s = piece_of(g, k);
+    const int s = pieces.of(k);
     if (!clip && g.src[s] == g.dst[s]) continue;
     const size_t at = (size_t)(k - g.first[s]) * g.ch, left = g.n[s] - at;
     const unsigned n = left < g.ch ? (unsigned)left : g.ch;

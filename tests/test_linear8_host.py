@@ -142,7 +142,7 @@ def test_rmsnorm8_grad_needs_its_workspace(ctx):
     L, h = ctx
     n = ctypes.c_size_t()
     assert L.jagg_rmsnorm8_grad(h, *GRAD.values()) == 1 and b"workspace" in L.jagg_last_error()
-    assert L.jagg_rmsnorm8_grad_bytes(8, 256, ctypes.byref(n)) == 0 and n.value >= 8 * 256 * 4
+    assert L.jagg_rmsnorm8_grad_bytes(8, 256, ctypes.byref(n)) == 0 and n.value >= 256 * 4
     assert L.jagg_ctx_set_workspace(h, P, n.value - 1) == 0
     assert L.jagg_rmsnorm8_grad(h, *GRAD.values()) == 1 and b"workspace" in L.jagg_last_error()
     assert L.jagg_rmsnorm8_grad_bytes(0, 256, ctypes.byref(n)) == 1 and L.jagg_rmsnorm8_grad_bytes(8, 256, None) == 1
