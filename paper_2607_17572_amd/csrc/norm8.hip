@@ -23,14 +23,33 @@ __device__ __forceinline__ float row_sum(float v, float* sh) {
   else return block_sum(v, sh);
 }
 
+// The same in fp64.
+template <int NT>
+__device__ __forceinline__ double row_sum64(double v, double* sh) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  if constexpr (NT > 64) {
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.0;
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) v += sh[i];
+  }
+  return v;
+}
+
+// The sum of squares is fp64 (the kernel waits for memory all the same), so that rstd is
+// off by its own rounding alone: an 8-bit value next to a border of its rounding then
+// falls to the exact side wherever fp32 factors can tell; and squares do not overflow.
 template <typename T, int NT, int NV>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm8_k(Norm8Args a) {
   constexpr int RPB = NT < 256 ? 256 / NT : 1;  // rows per workgroup
-  __shared__ float sh[16];
+  __shared__ double sh[16];
   const int t = threadIdx.x % NT, row = blockIdx.x * RPB + threadIdx.x / NT;
   if (row >= a.rows) return;  // whole waves: RPB > 1 only with NT = 64, which has no barrier
   const T* x = (const T*)a.x + (size_t)row * a.ldx;
-  float v[NV][8], ss = 0.f;
+  float v[NV][8];
+  double ss = 0.0;
 #pragma unroll
   for (int i = 0; i < NV; ++i) load8(x, 8 * (i * NT + t), a.cols, v[i]);
   if (a.r) {
@@ -55,9 +74,9 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm8_k(Norm8Args a) {
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ss = fmaf(v[i][e], v[i][e], ss);
-  ss = row_sum<NT>(ss, sh);
-  const float rstd = 1.f / sqrtf(ss / (float)a.cols + a.eps);
+    for (int e = 0; e < 8; ++e) ss = fma((double)v[i][e], (double)v[i][e], ss);
+  ss = row_sum64<NT>(ss, sh);
+  const float rstd = (float)(1.0 / sqrt(ss / a.cols + a.eps));
   if (a.rstd && t == 0) a.rstd[row] = rstd;
   uint8_t* q = a.y.q + (size_t)row * a.y.ld;
   const int kp = (a.cols + 127) / 128 * 128;
