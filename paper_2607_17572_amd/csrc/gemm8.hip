@@ -814,7 +814,7 @@ enum Kind8 { K8_FEW, K8_64, K8_128, K8_256 };
 // four splits: 15.0).
 
 size_t matmul8_plan(Matmul8Args& g) {
-  const int M = g.a.rows, N = g.b.rows, nb = (g.a.k + 127) / 128;
+  const int M = g.a.rows, N = g.b.rows, nb = (int)(((long)g.a.k + 127) / 128);
   g.kind = K8_FEW;
   g.splits = 1;
   g.per_split = nb;
@@ -823,7 +823,7 @@ size_t matmul8_plan(Matmul8Args& g) {
   double bt = 1e300;
   for (int kind = K8_64; kind <= K8_256; ++kind) {
     const int b = kind == K8_64 ? 64 : kind == K8_128 ? 128 : 256;
-    const long tiles = (long)((M + b - 1) / b) * ((N + b - 1) / b);
+    const long tiles = ((long)M + b - 1) / b * (((long)N + b - 1) / b);
     for (int s = 1; s <= 16; ++s) {
       const int ps = s == 1 ? nb : ((nb + s - 1) / s + 3) / 4 * 4;
       const long wgs = tiles * s;

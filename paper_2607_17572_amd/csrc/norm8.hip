@@ -146,8 +146,8 @@ static int norm8_threads(int cols, int dt) {
   return cols <= (dt == BF16 ? 4096 : 2048) ? 64 : cols <= 8192 ? 256 : 1024;
 }
 static int norm8_workgroups(int rows, int cols, int dt) {
-  const int per = norm8_threads(cols, dt) == 64 ? 4 : 1, want = (rows + per - 1) / per;
-  return want < 512 ? want : 512;
+  const int per = norm8_threads(cols, dt) == 64 ? 4 : 1;
+  return (int)std::min(((long)rows + per - 1) / per, 512l);
 }
 size_t rmsnorm8_grad_bytes(int rows, int cols) {
   const size_t w = std::max(norm8_workgroups(rows, cols, BF16), norm8_workgroups(rows, cols, F32));
@@ -170,8 +170,8 @@ template <typename T, bool V8>
 struct Row8 {
   T* p;
   int cols;
-  __device__ __forceinline__ Row8(const void* m, size_t ld, int row, int n) {
-    p = m ? (T*)m + (size_t)row * ld : nullptr;
+  __device__ __forceinline__ Row8(const void* m, size_t ld, unsigned row, int n) {
+    p = m ? (T*)m + row * ld : nullptr;
     cols = m ? n : 0;
   }
 };
@@ -240,7 +240,8 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm8_grad_k(Norm8Grad
   __shared__ float sh[16];
   __shared__ __attribute__((aligned(16))) float sum[WAVE ? 512 * NV : 1];
   __shared__ __attribute__((aligned(16))) T gain[WAVE ? 512 * NV : 1];  // as the lanes hold it
-  const int t = threadIdx.x % NT, sub = WAVE ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0, workers = gridDim.x * RPB;
+  const int t = threadIdx.x % NT, sub = WAVE ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
+  const unsigned workers = gridDim.x * RPB;
   Raw8<T, V8> g[WAVE ? 1 : NV];
   float dg[NV][8];
   if constexpr (WAVE) {
@@ -255,7 +256,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm8_grad_k(Norm8Grad
 #pragma unroll
     for (int e = 0; e < 8; ++e) dg[i][e] = 0.f;
   const float inv_c = 1.f / (float)a.cols;
-  for (int row = blockIdx.x * RPB + sub; row < a.rows; row += workers) {
+  for (unsigned row = blockIdx.x * RPB + sub; row < (unsigned)a.rows; row += workers) {
     Raw8<T, V8> dy[NV], h[NV], dh[NV];
     const Row8<T, V8> rdy(a.dy, a.lddy, row, a.cols), rh(a.h, a.ldh, row, a.cols), rdh(a.dh, a.lddh, row, a.cols),
         rdx(a.dx, a.lddx, row, a.cols);

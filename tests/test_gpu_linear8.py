@@ -245,6 +245,30 @@ def test_matmul8_carries_nan_and_zero_blocks(ctx):
     assert not bool(out[:5].isnan().any()) and not bool(out[6:].isnan().any())
 
 
+@pytest.mark.parametrize("m,n,k", [(3, 40, 700), (70, 50, 700), (200, 300, 1500), (2100, 2100, 400), (4200, 4200, 300), (40, 300, 9000)])
+@pytest.mark.parametrize("dt", [BF, FP])
+def test_matmul8_takes_exponent_255_as_nan_and_0_as_the_least(ctx, m, n, k, dt):
+    """Whatever the bytes of a block are: exponent 255 makes its row (or column) of the
+    result NaN; exponent 0 scales by 2^-127."""
+    say(f"case: matmul8 exponents {m}x{n}x{k} {dt}")
+    a, va = whole_mat(m, m, k, "e4m3", 0)
+    b, vb = whole_mat(n, n, k, "e4m3", 0)
+    a.scale[0, 2, 1], b.scale[0, 7, 0] = 255, 255
+    a.scale[:, 0, :] = 0
+    b.scale[:, 5, :] = 254  # 2^127 (2^-127) = 1
+    out = torch.empty(m, n, dtype=dt, device="cuda")
+    ctx.matmul8(a, b, out)
+    got = f64(out)
+    # (column 5 of the other rows is whole numbers times 2^127: past fp32's largest, 2^128)
+    rest = np.delete(got, 5, axis=1)
+    assert np.isnan(got[2]).all() and np.isnan(got[:, 7]).all() and np.isnan(rest).sum() == m + n - 2
+    fine = [i for i in range(min(m, 60)) if i not in (0, 2)]
+    cols = [j for j in range(min(n, 60)) if j not in (5, 7)]
+    assert np.array_equal(got[np.ix_(fine, cols)], f64(torch.from_numpy(va[fine] @ vb[cols].T).to(dt)))
+    if dt is BF:
+        assert got[0, 5] == f64(torch.tensor(float(va[0] @ vb[5])).to(dt))
+
+
 @pytest.mark.parametrize("m", [2, 33, 300000])
 def test_matmul8_operands_past_4_gib(ctx, m):
     """Offsets of the last rows lie past 32 bits: on the left with many rows, on the
@@ -470,6 +494,37 @@ def test_a_layers_step_in_a_graph():
             s.synchronize()
             for k, v in out.items():
                 assert torch.equal(v.q if isinstance(v, pk.Mat8) else v, want[k]), (i, k)
+
+
+def test_a_first_call_inside_a_capture():
+    """A context whose first calls are captured (its workspace is made and grows there),
+    then used eagerly and replayed."""
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        one, two = (pk.Context(pk.config("tiny"), stream=s) for _ in range(2))
+        t, out = layer_state(333, 520, 1000)
+        big = layer_state(2000, 3000, 256)
+        other = layer_state(50, 4000, 64)
+        for st in (t, big[0], other[0]):
+            weights(two, st)
+        layer(two, t, out)
+        layer(two, *big)
+        s.synchronize()
+        want = {k: (v.q if isinstance(v, pk.Mat8) else v).clone() for k, v in out.items()}
+        want_big = big[1]["dw"].clone()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            layer(one, t, out)
+            layer(one, *big)
+        for _ in range(3):
+            for v in out.values():
+                (v.q if isinstance(v, pk.Mat8) else v).zero_()
+            layer(one, *other)
+            g.replay()
+            s.synchronize()
+            for k, v in out.items():
+                assert torch.equal(v.q if isinstance(v, pk.Mat8) else v, want[k]), k
+            assert torch.equal(big[1]["dw"], want_big)
 
 
 def test_workspace_of_a_graph_outlives_a_larger_call():
