@@ -14,6 +14,15 @@ BF, FP, DB = torch.bfloat16, torch.float32, torch.float64
 INF = float("inf")
 
 
+@pytest.fixture(autouse=True)
+def fp32_default():
+    """Another test file sets fp64 as the default type."""
+    was = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(was)
+
+
 @pytest.fixture(scope="module")
 def ctx():
     return pk.Context(pk.config("tiny"))

@@ -17,6 +17,15 @@ FMT = {"e4m3": pk.E4M3, "e5m2": pk.E5M2}
 MARGIN = 4096
 
 
+@pytest.fixture(autouse=True)
+def fp32_default():
+    """Another test file sets fp64 as the default type."""
+    was = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(was)
+
+
 @pytest.fixture(scope="module")
 def ctx():
     return pk.Context(pk.config("tiny"))

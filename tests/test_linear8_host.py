@@ -13,6 +13,15 @@ P = 1 << 20  # a fake, aligned device address: never dereferenced
 NAN, INF = float("nan"), float("inf")
 
 
+@pytest.fixture(autouse=True)
+def fp32_default():
+    """Another test file sets fp64 as the default type."""
+    was = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(was)
+
+
 @pytest.fixture()
 def ctx():
     L = _lib_or_skip()
