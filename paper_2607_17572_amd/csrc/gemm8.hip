@@ -541,7 +541,66 @@ __device__ __forceinline__ void quarter_sched() {
   }
 }
 
-template <int FA, int BM, int BN, int L2, int L3>
+// Epilogue of the streaming form: a wave's fragments by 32 rows x 64 columns through 4.5 KB
+// of LDS of its own, already rounded (the bias is added in the accumulators' layout: a
+// lane holds four neighbouring columns of a row).  Bs: the bias from col0 on, in LDS.
+// N % 8 == 0, beta 0.
+template <int SM, int SN>
+__device__ __forceinline__ void store_stream(const Matmul8Args& g, f32x16 (&acc)[SM][SN], int row0, int col0, const uint16_t* Bs,
+                                             uint16_t* Ts) {
+  constexpr int CS = 72;  // bf16 per staged row
+  int lane = threadIdx.x & 63;
+  long ldo = g.ldo;
+  asm volatile("" : "+v"(lane), "+s"(ldo));  // nothing of the epilogue is kept in registers over the products
+  const int l = lane & 31, h = lane >> 5, r8 = lane >> 3, c8 = (lane & 7) * 8, M = g.a.rows, N = g.b.rows;
+  uint16_t* const out = (uint16_t*)g.out + (size_t)(row0 + r8) * ldo + col0 + c8;
+#pragma unroll
+  for (int jj = 0; jj < SN; jj += 2) {
+    __builtin_amdgcn_sched_barrier(0);
+    float b[2][16];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint2 w = *(const uint2*)(Bs + 32 * (jj + j) + 8 * q + 4 * h);
+        b[j][4 * q] = __uint_as_float(w.x << 16);
+        b[j][4 * q + 1] = __uint_as_float(w.x & 0xffff0000u);
+        b[j][4 * q + 2] = __uint_as_float(w.y << 16);
+        b[j][4 * q + 3] = __uint_as_float(w.y & 0xffff0000u);
+      }
+#pragma unroll
+    for (int i = 0; i < SM; ++i) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t o[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int n = 4 * q + 2 * e;
+            o[e] = (uint32_t)f2bf(acc[i][jj + j][n] + b[j][n]) | (uint32_t)f2bf(acc[i][jj + j][n + 1] + b[j][n + 1]) << 16;
+          }
+          *(uint2*)(Ts + l * CS + 32 * j + 8 * q + 4 * h) = make_uint2(o[0], o[1]);
+        }
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const u32x4a o = *(const u32x4a*)(Ts + (8 * p + r8) * CS + c8);
+        if (row0 + 32 * i + 8 * p + r8 < M && col0 + 32 * jj + c8 < N)
+          *(u32x4a*)(out + (size_t)(32 * i + 8 * p) * ldo + 32 * jj) = o;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+
+// STREAM: at most one workgroup per CU goes through the tiles id, id + grid, ...; the last
+// two k tiles of one load the first two of the next, so that its first operands are in
+// registers before the epilogue, which has its own LDS, and its loads fly meanwhile.
+// Without it a workgroup waits 2 us for its first tile and 3 for its last stores.
+// 9216 x 12288, k 512: 113 -> 95 us; 9216 x 16384, k 4096 with bias 474 -> 465 (loading the
+// bias from memory in the epilogue 472: a wait for it is one for the loads before it).
+template <int FA, int BM, int BN, int L2, int L3, bool STREAM>
 __global__ __launch_bounds__(256) void matmul8_quad_k(Matmul8Args g) {
   take_split(g);
   constexpr int BK = 128, SM = BM / 64, SN = BN / 64, HM = SM / 2, HN = SN / 2;  // 32 x 32 fragments of a wave
@@ -551,9 +610,15 @@ __global__ __launch_bounds__(256) void matmul8_quad_k(Matmul8Args g) {
 
   const int M = g.a.rows, N = g.b.rows;
   const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
-  int tm, tn;
-  tile_coords(xcd_remap(blockIdx.x, tiles_m * tiles_n), tiles_m, tiles_n, tm, tn);
-  const int m0 = tm * BM, n0 = tn * BN;
+  const int tiles = tiles_m * tiles_n;
+  auto place = [&](int id, int& m, int& n) {
+    int tm, tn;
+    tile_coords(xcd_remap(id, tiles), tiles_m, tiles_n, tm, tn);
+    m = tm * BM;
+    n = tn * BN;
+  };
+  int id = blockIdx.x, m0, n0, m1 = 0, n1 = 0;  // this tile and (STREAM) the next one
+  place(id, m0, n0);
   const int lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
 
@@ -566,32 +631,45 @@ __global__ __launch_bounds__(256) void matmul8_quad_k(Matmul8Args g) {
   // the tile's rows: offsets stay below 2^31 (ld <= 2^22), rows past the end and the
   // prefetch behind the last row read zeros
   const int nk = (g.a.k + BK - 1) / BK;
-  const __amdgpu_buffer_rsrc_t RA = make_rsrc(g.a.q + (size_t)m0 * g.a.ld, (min(BM, M - m0) - 1) * (long)g.a.ld + nk * BK);
-  const __amdgpu_buffer_rsrc_t RB = make_rsrc(g.b.q + (size_t)n0 * g.b.ld, (min(BN, N - n0) - 1) * (long)g.b.ld + nk * BK);
+  bool more = false;  // there is a next tile: otherwise its loads bring nothing
+#define JG_ROWS8(x, r0, cnt, on) \
+  make_rsrc(x.q + (size_t)(r0) * x.ld, (on) ? (min(cnt, x.rows - (r0)) - 1) * (long)x.ld + nk * BK : 0)
+  __amdgpu_buffer_rsrc_t RA = JG_ROWS8(g.a, m0, BM, true), RB = JG_ROWS8(g.b, n0, BN, true);
 
   // exponent words of the tile's rows, four k tiles each: through LDS as well
   __shared__ __attribute__((aligned(256))) uint32_t stw[BM + BN];
   constexpr int NWL = (BM + BN) / 256;  // direct loads of 64 words per wave
+  constexpr int NW = NWL + STREAM;      // and one of the bias
+  __shared__ __attribute__((aligned(256))) uint32_t stb[STREAM ? 256 : 1];
+  static_assert(BN <= 512, "a wave's 64 words of two columns");
   uint32_t wa[SM], wb[SN];
-  auto load_words = [&](int t) {  // of k tile t (a multiple of 4); the last ones again behind the end
+  // of k tile t (a multiple of 4) of the tile at m, n; the last ones again behind the end
+  auto load_words = [&](int t, int m, int n, bool on) {
     const size_t w = min(t, nk - 1) / 4;
 #pragma unroll
     for (int i = 0; i < NWL; ++i) {
       const int row = 64 * (4 * i + wave);  // of A's rows, then B's
-      const bool a = row < BM;
+      const bool a = BM >= 256 ? i < BM / 256 : wave < BM / 64;
+      const int rows = a ? M : N, r0 = a ? m : n;
       const __amdgpu_buffer_rsrc_t W =
-          a ? make_rsrc(g.a.sc + w * M + m0, min(BM, M - m0) * 4) : make_rsrc(g.b.sc + w * N + n0, min(BN, N - n0) * 4);
+          make_rsrc((a ? g.a.sc : g.b.sc) + w * rows + r0, on ? min(a ? BM : BN, rows - r0) * 4 : 0);
       load_lds4(W, (char*)(stw + row), ((a ? row : row - BM) + lane) * 4);
     }
   };
 
   f32x16 acc[SM][SN];
+  auto clear = [&]() {
 #pragma unroll
-  for (int i = 0; i < SM; ++i)
+    for (int i = 0; i < SM; ++i)
 #pragma unroll
-    for (int j = 0; j < SN; ++j)
+      for (int j = 0; j < SN; ++j) {
+        float z = 0.f;
+        if constexpr (STREAM) asm volatile("" : "+v"(z));  // or one fragment of zeros is kept and copied
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = z;
+      }
+  };
+  clear();
 
   i32x8 fa[SM][2], fb[SN][2];
   auto read_a = [&](const char* S, int half, bool w) {  // w: the exponent words too
@@ -622,20 +700,20 @@ __global__ __launch_bounds__(256) void matmul8_quad_k(Matmul8Args g) {
                                                                       (int)wa[i]);
   };
 
-  // direct loads LO .. HI - 1 of k tile t (A's, then B's)
-  auto load = [&](auto lo, auto hi, char* S, int t) {
+  // direct loads LO .. HI - 1 (A's, then B's) of k tile t
+  auto load = [&](auto lo, auto hi, const __amdgpu_buffer_rsrc_t& A, const __amdgpu_buffer_rsrc_t& B, char* S, int t) {
     constexpr int LO = decltype(lo)::value, HI = decltype(hi)::value, NA = OpA::NL;
-    if constexpr (LO < NA) oa.template load<LO, (HI < NA ? HI : NA) - LO>(RA, S, t * BK);
-    if constexpr (HI > NA) ob.template load<(LO > NA ? LO - NA : 0), HI - (LO > NA ? LO : NA)>(RB, S + SB, t * BK);
+    if constexpr (LO < NA) oa.template load<LO, (HI < NA ? HI : NA) - LO>(A, S, t * BK);
+    if constexpr (HI > NA) ob.template load<(LO > NA ? LO - NA : 0), HI - (LO > NA ? LO : NA)>(B, S + SB, t * BK);
   };
   constexpr int NL = OpA::NL + OpB::NL;
   typedef std::integral_constant<int, 0> C0;
   typedef std::integral_constant<int, NL * L2 / 16> C1;
   typedef std::integral_constant<int, NL * (L2 + L3) / 16> C2;
   typedef std::integral_constant<int, NL> C3;
-  load_words(0);
-  load(C0(), C3(), st0, 0);
-  load(C0(), C3(), st1, 1);
+  load_words(0, m0, n0, true);
+  load(C0(), C3(), RA, RB, st0, 0);
+  load(C0(), C3(), RA, RB, st1, 1);
   wait_vm_lds<NL>();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
@@ -643,13 +721,17 @@ __global__ __launch_bounds__(256) void matmul8_quad_k(Matmul8Args g) {
   read_b(st0, 0, true);
 
   constexpr int MF = 2 * HM * HN;
-  auto iter = [&](auto cc, int kt) {
+  // one k tile; loads the k tile t2 of A, B into its place and, in the second of four, the
+  // words of k tile tw of the tile at mw, nw
+  auto iter = [&](auto cc, const __amdgpu_buffer_rsrc_t& A, const __amdgpu_buffer_rsrc_t& B, int t2, int tw = 0, int mw = 0,
+                  int nw = 0, bool on = true) __attribute__((always_inline)) {
     constexpr int c = decltype(cc)::value, p = c & 1;
     char* S = p ? st1 : st0;
     const char* Sn = p ? st0 : st1;
     // keeps the fragments' addresses (too far apart for one base) from being held in
     // registers over the loop: an addition each instead
     asm("" : "+v"(oa.fo), "+v"(ob.fo));
+    if constexpr (STREAM) asm("" : "+v"(oa.voff), "+v"(ob.voff), "+s"(oa.step), "+s"(ob.step));
     read_b(S, 1 - p, c == 0);
     read_a(S, 1, c == 0);
     quarter(cc, 0, p);
@@ -660,43 +742,81 @@ __global__ __launch_bounds__(256) void matmul8_quad_k(Matmul8Args g) {
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    load(C0(), C1(), S, kt + 2);
+    load(C0(), C1(), A, B, S, t2);
     quarter(cc, 0, 1 - p);
     quarter_sched<MF, 0, C1::value, 1>();
     __builtin_amdgcn_sched_barrier(0);
     // (the words of the four k tiles under way are in registers since the first of them)
-    if constexpr (c == 1) load_words(kt + 3);
-    load(C1(), C2(), S, kt + 2);
+    if constexpr (c == 1) load_words(tw, mw, nw, on);
+    if constexpr (c == 1 && STREAM)  // this tile's bias, zeros if there is none
+      load_lds4(make_rsrc((const uint16_t*)g.bias + n0, g.bias ? min(BN, N - n0) * 2 : 0), (char*)(stb + 64 * wave), threadIdx.x * 4);
+    load(C1(), C2(), A, B, S, t2);
     quarter(cc, 1, 1 - p);
-    quarter_sched<MF, 0, C2::value - C1::value + (c == 1 ? NWL : 0), 1>();
+    quarter_sched<MF, 0, C2::value - C1::value + (c == 1 ? NW : 0), 1>();
     __builtin_amdgcn_sched_barrier(0);
     // the next k tile has landed once only the loads of the one after it (and the words) fly
-    wait_vm_lds<C2::value + (c == 1 ? NWL : 0)>();
+    wait_vm_lds<C2::value + (c == 1 ? NW : 0)>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    load(C2(), C3(), S, kt + 2);
+    load(C2(), C3(), A, B, S, t2);
     read_a(Sn, 0, c == 3);
     read_b(Sn, 1 - p, c == 3);
     quarter(cc, 1, p);
     quarter_sched<MF, (c == 3 ? 5 : 4) * (HM + HN), NL - C2::value, 3>();
     __builtin_amdgcn_sched_barrier(0);
   };
-  int kt = 0;
-  for (; kt + 3 < nk; kt += 4) {
-    iter(std::integral_constant<int, 0>(), kt);
-    iter(std::integral_constant<int, 1>(), kt + 1);
-    iter(std::integral_constant<int, 2>(), kt + 2);
-    iter(std::integral_constant<int, 3>(), kt + 3);
+  typedef std::integral_constant<int, 0> I0;
+  typedef std::integral_constant<int, 1> I1;
+  typedef std::integral_constant<int, 2> I2;
+  typedef std::integral_constant<int, 3> I3;
+  const int row_in = wm * (BM / 2), col_in = wn * (BN / 2);
+  if constexpr (STREAM) {
+    __shared__ __attribute__((aligned(16))) uint16_t ste[4][32 * 72];
+    for (;;) {
+      more = id + (int)gridDim.x < tiles;
+      if (more) {
+        id += gridDim.x;
+        place(id, m1, n1);
+      }
+      const __amdgpu_buffer_rsrc_t RA1 = JG_ROWS8(g.a, m1, BM, more), RB1 = JG_ROWS8(g.b, n1, BN, more);
+      int kt = 0;
+      do {
+        const bool end = kt + 4 >= nk;
+        const __amdgpu_buffer_rsrc_t A = end ? RA1 : RA, B = end ? RB1 : RB;
+        const int t = end ? 0 : kt + 4;
+        iter(I0(), RA, RB, kt + 2);
+        iter(I1(), RA, RB, kt + 3, t, end ? m1 : m0, end ? n1 : n0, !end || more);
+        iter(I2(), A, B, t);
+        iter(I3(), A, B, t + 1);
+        kt += 4;
+      } while (kt < nk);
+      store_stream<SM, SN>(g, acc, m0 + row_in, n0 + col_in, (const uint16_t*)stb + col_in, ste[wave]);
+      if (!more) break;
+      clear();
+      m0 = m1;
+      n0 = n1;
+      RA = RA1;
+      RB = RB1;
+    }
+    __builtin_amdgcn_s_waitcnt(0);  // no load into LDS outlives the workgroup
+  } else {
+    int kt = 0;
+    for (; kt + 3 < nk; kt += 4) {
+      iter(I0(), RA, RB, kt + 2);
+      iter(I1(), RA, RB, kt + 3, kt + 4, m0, n0);
+      iter(I2(), RA, RB, kt + 4);
+      iter(I3(), RA, RB, kt + 5);
+    }
+    if (kt < nk) iter(I0(), RA, RB, kt + 2);
+    if (kt + 1 < nk) iter(I1(), RA, RB, kt + 3, kt + 4, m0, n0);
+    if (kt + 2 < nk) iter(I2(), RA, RB, kt + 4);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    constexpr int TB = 4 * epi_floats<SN>();
+    static_assert(2 * TB <= (BM + BN) * BK, "epilogue staging");
+    epilogue8<uint16_t, SM, SN>(g, acc, m0 + row_in, n0 + col_in, (float*)((wave & 2 ? st1 : st0) + (wave & 1) * TB));
   }
-  if (kt < nk) iter(std::integral_constant<int, 0>(), kt);
-  if (kt + 1 < nk) iter(std::integral_constant<int, 1>(), kt + 1);
-  if (kt + 2 < nk) iter(std::integral_constant<int, 2>(), kt + 2);
-  __builtin_amdgcn_s_waitcnt(0);
-  __syncthreads();
-
-  constexpr int TB = 4 * epi_floats<SN>();
-  static_assert(2 * TB <= (BM + BN) * BK, "epilogue staging");
-  epilogue8<uint16_t, SM, SN>(g, acc, m0 + wm * (BM / 2), n0 + wn * (BN / 2), (float*)((wave & 2 ? st1 : st0) + (wave & 1) * TB));
+#undef JG_ROWS8
 }
 
 // ------------------------------------------------------------------- few rows
@@ -786,10 +906,19 @@ __global__ __launch_bounds__(256) void matmul8_join_k(Matmul8Args g) {
   store_c<T, 4>(g, (int)row, col, v);
 }
 
+// The streaming form of 256 x 256 tiles: whole groups of four k tiles, 16-byte stores
+static bool streams(const Matmul8Args& g) { return ((long)g.a.k + 127) / 128 % 4 == 0 && g.b.rows % 8 == 0; }
+
 template <int FA, int BM, int BN>
 static void launch_quad(const Matmul8Args& g, hipStream_t s) {
   const dim3 grid((unsigned)((g.a.rows + BM - 1) / BM) * (unsigned)((g.b.rows + BN - 1) / BN), g.splits);
-  hipLaunchKernelGGL((matmul8_quad_k<FA, BM, BN, 6, 5>), grid, dim3(256), 0, s, g);
+  if constexpr (BM == 256) {
+    if (g.splits == 1 && streams(g) && (uintptr_t)g.bias % 4 == 0 && g.beta == 0.f) {
+      hipLaunchKernelGGL((matmul8_quad_k<FA, BM, BN, 6, 5, true>), dim3(grid.x < 256 ? grid.x : 256), dim3(256), 0, s, g);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((matmul8_quad_k<FA, BM, BN, 6, 5, false>), grid, dim3(256), 0, s, g);
 }
 
 template <int FA, typename T, int BM, int BN, int WM, int WN, int KG>
@@ -805,9 +934,10 @@ enum Kind8 { K8_FEW, K8_64, K8_128, K8_256 };
 // of 128 of a split x time per block + prologue and epilogue), and for a split the
 // second launch and the sums' way through memory.  The times per block are those
 // measured with every CU busy: bf16 0.25 (64 x 64), 0.58 (128 x 128; 1.0 for two on a
-// CU), 1.4 (256 x 256); fp32 0.29, 0.78 (1.65), 3.2.  Over 110 sizes drawn from 17 .. 9216
+// CU), 1.4 (256 x 256); fp32 0.29, 0.78 (1.65), 3.2.  (8192 x 8192, k 512: 79 us in 128 x 128
+// tiles, 62 in 256 x 256; 6144 x 6144, k 1024: 50, 52.)  Over 200 sizes drawn from 17 .. 9216
 // rows, 64 .. 16384 columns and k the choice takes 1.00 times the best of three
-// tiles x eight splits in the mean and 1.17 times at most.  Examples (us; 64 x 64 in one
+// tiles x eight splits in the mean and 1.19 times at most.  Examples (us; 64 x 64 in one
 // and four splits, 128 x 128 in one and eight, bf16): 37 x 4096, k 12288: 34, 16, 59, 17;
 // 128 rows: 34, 27, 63, 22; 1024 x 1024, k 4096: 12, 22, 18, -; 1024 x 4096, k 4096: 37, 64,
 // 20, -.  The single-token kernel up to 16 rows: 13.8 at 16 x 4096, k 12288 (64 x 64 tiles in
@@ -837,7 +967,7 @@ size_t matmul8_plan(Matmul8Args& g) {
         const long rest = wgs % 512;
         t = 2.0 + wgs / 512 * two + (rest == 0 ? 0.0 : rest <= 256 ? one : two);
       } else {
-        t = 4.0 + (wgs + 255) / 256 * (ps * (f32 ? 3.2 : 1.4) + 8.5);
+        t = 4.0 + (wgs + 255) / 256 * (ps * (f32 ? 3.2 : 1.4) + (s == 1 && streams(g) ? 6.5 : 8.5));
       }
       if (s > 1) t += 4.0 + (double)M * N * s * 8 / 4.5e6;
       if (t < bt) {

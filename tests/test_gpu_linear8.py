@@ -220,6 +220,32 @@ def test_matmul8_with_a_split_contraction(m, n, k, dt):
     assert bool((out[:, 0] == 3).all()) and bool((out[:, n + 1] == 3).all())
 
 
+@pytest.mark.parametrize("m,n,k,fmt", [(4096, 4096, 500, "e4m3"), (5000, 5000, 2048, "e5m2"), (5000, 5001, 1990, "e4m3"),
+                                       (8200, 8200, 512, "e4m3"), (16000, 2056, 1024, "e5m2")])
+def test_matmul8_with_more_tiles_than_compute_units(ctx, m, n, k, fmt):
+    """bf16 results: a workgroup goes from tile to tile.  Rows of a wider buffer; a bias at
+    an odd place and accumulation (which take a workgroup per tile) give the same."""
+    say(f"case: matmul8 many tiles {m}x{n}x{k} {fmt}")
+    a, va = whole_mat(m, m, k, fmt, 1)
+    b, vb = whole_mat(n + 1, n, k, "e4m3", 1)
+    assert np.abs(va).sum(1).max() * np.abs(vb).max() < 2 ** 24
+    want = torch.from_numpy(va.astype(np.float32) @ vb.astype(np.float32).T)  # whole numbers below 2^24: exact
+    bias = torch.arange(n + 1, dtype=FP).remainder(5).to(BF).cuda()
+    out = torch.full((m, n + 3), 7.0, dtype=BF, device="cuda")
+    mid = out[:, 1:n + 1]
+    ctx.matmul8(a, b, mid)
+    assert torch.equal(mid.cpu(), want.to(BF))
+    for at in (0, 1):
+        mid.fill_(3)
+        ctx.matmul8(a, b, mid, bias=bias[at:at + n])
+        wanted = (want + bias[at:at + n].float().cpu()).to(BF)
+        assert torch.equal(mid.cpu(), wanted), at
+    mid.fill_(2)
+    ctx.matmul8(a, b, mid, bias=bias[1:], beta=1.0)
+    assert torch.equal(mid.cpu(), (want + bias[1:].float().cpu() + 2).to(BF))
+    assert bool((out[:, 0] == 7).all()) and bool((out[:, n + 1:] == 7).all())
+
+
 @pytest.mark.parametrize("m,n,k,fmt", [(1, 300, 3000, "e4m3"), (5, 129, 8200, "e5m2"), (40, 200, 2000, "e4m3"),
                                        (200, 333, 2500, "e5m2"), (600, 700, 1100, "e4m3")])
 def test_matmul8_on_quantised_values(ctx, m, n, k, fmt):
