@@ -928,20 +928,22 @@ static void launch_tile(const Matmul8Args& g, hipStream_t s) {
 }
 
 // ---------------------------------------------------------------------- launch
-enum Kind8 { K8_FEW, K8_64, K8_128, K8_256 };
+enum Kind8 { K8_FEW, K8_32, K8_64, K8_128, K8_256 };
 
 // Tiles and splits of k: the least estimated time (us) = rounds of the 256 CUs x (blocks
 // of 128 of a split x time per block + prologue and epilogue), and for a split the
 // second launch and the sums' way through memory.  The times per block are those
 // measured with every CU busy: bf16 0.25 (64 x 64), 0.58 (128 x 128; 1.0 for two on a
-// CU), 1.4 (256 x 256); fp32 0.29, 0.78 (1.65), 3.2.  (8192 x 8192, k 512: 79 us in 128 x 128
-// tiles, 62 in 256 x 256; 6144 x 6144, k 1024: 50, 52.)  Over 200 sizes drawn from 17 .. 9216
-// rows, 64 .. 16384 columns and k the choice takes 1.00 times the best of three
-// tiles x eight splits in the mean and 1.19 times at most.  Examples (us; 64 x 64 in one
-// and four splits, 128 x 128 in one and eight, bf16): 37 x 4096, k 12288: 34, 16, 59, 17;
-// 128 rows: 34, 27, 63, 22; 1024 x 1024, k 4096: 12, 22, 18, -; 1024 x 4096, k 4096: 37, 64,
-// 20, -.  The single-token kernel up to 16 rows: 13.8 at 16 x 4096, k 12288 (64 x 64 tiles in
-// four splits: 15.0).
+// CU), 1.4 (256 x 256); fp32 0.29, 0.78 (1.65), 3.2.  64 x 32 tiles, each of four groups of
+// waves with a quarter of k, need no second launch but read the left operand twice as
+// often: 0.42 per block of a group on up to 32 CUs, 0.5 (17 rows) to 0.78 (64) above, 1 in
+// more than one round.  Over 320 sizes drawn from 17 .. 9000 rows, 64 .. 16384 columns and k
+// the choice takes 0.99 times the best of four tiles x eight splits in the mean and 1.22
+// times at most.  Examples (us, bf16; 64 x 32, 64 x 64 in one and four splits, 128 x 128):
+// 37 x 4096, k 12288: 21, 32, 16, 78; 18 x 7040, k 4864: 9.9, 12, 13, 20; 31 x 326, k 5248: 7.6,
+// 9.3, 10, 17; 1024 x 4096, k 4096: -, 37, 64, 20; 8192 x 8192, k 512: 128 x 128 79, 256 x 256
+// 62; 6144 x 6144, k 1024: 50, 52.  The single-token kernel up to 16 rows: 13.8 at 16 x 4096,
+// k 12288 (64 x 64 tiles in four splits: 15.0).
 
 size_t matmul8_plan(Matmul8Args& g) {
   const int M = g.a.rows, N = g.b.rows, nb = (int)(((long)g.a.k + 127) / 128);
@@ -951,16 +953,20 @@ size_t matmul8_plan(Matmul8Args& g) {
   if (M <= 16) return 0;
   const bool f32 = g.out_dt == F32;
   double bt = 1e300;
-  for (int kind = K8_64; kind <= K8_256; ++kind) {
-    const int b = kind == K8_64 ? 64 : kind == K8_128 ? 128 : 256;
-    const long tiles = ((long)M + b - 1) / b * (((long)N + b - 1) / b);
+  for (int kind = K8_32; kind <= K8_256; ++kind) {
+    const int b = kind <= K8_64 ? 64 : kind == K8_128 ? 128 : 256, bn = kind == K8_32 ? 32 : b;
+    const long tiles = ((long)M + b - 1) / b * (((long)N + bn - 1) / bn);
     for (int s = 1; s <= 16; ++s) {
       const int ps = s == 1 ? nb : ((nb + s - 1) / s + 3) / 4 * 4;
       const long wgs = tiles * s;
       if (s > 1 && (ps < 8 || wgs > 1024)) break;  // more only costs more
       if ((nb + ps - 1) / ps != s) continue;
       double t;
-      if (kind == K8_64) {
+      if (kind == K8_32) {
+        if (s > 1) break;  // its four groups of k are the split
+        const double one = wgs > 256 ? 1.0 : wgs > 32 ? 0.5 + 0.006 * ((M < 64 ? M : 64) - 17) : 0.42;
+        t = 2.8 + (wgs + 255) / 256 * ((nb + 15) / 16 * 4 * (f32 ? 1.25 : 1.0) * one);
+      } else if (kind == K8_64) {
         t = 2.0 + (wgs + 255) / 256 * (ps * (f32 ? 0.29 : 0.25) + 1.5);
       } else if (kind == K8_128) {  // two workgroups per CU
         const double one = ps * (f32 ? 0.78 : 0.58) + 2.5, two = ps * (f32 ? 1.65 : 1.0) + 3.5;
@@ -987,6 +993,7 @@ static void launch_matmul8(const Matmul8Args& g, hipStream_t s) {
     hipLaunchKernelGGL((matmul8_few_k<FA, T>), dim3((g.b.rows + 15) / 16), dim3(512), 0, s, g);
     return;
   }
+  if (g.kind == K8_32) return launch_tile<FA, T, 64, 32, 1, 1, 4>(g, s);
   if (g.kind == K8_64) return launch_tile<FA, T, 64, 64, 1, 2, 2>(g, s);
   if constexpr (sizeof(T) == 2) {
     if (g.kind == K8_128) launch_quad<FA, 128, 128>(g, s);

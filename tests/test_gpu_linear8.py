@@ -210,6 +210,7 @@ def test_matmul8_with_a_split_contraction(m, n, k, dt):
     out = torch.full((m, n + 2), 3.0, dtype=dt, device="cuda")
     bias = torch.arange(n, dtype=FP).remainder(7).to(dt).cuda()
     ctx.matmul8(a, b, out[:, 1:n + 1])
+    ctx._ensure_bytes(1)  # (129 rows in bf16 need none: four groups of k in a workgroup)
     ctx._ws.view(torch.uint8).fill_(0xFF)
     ctx.matmul8(a, b, out[:, 1:n + 1], bias=bias)
     want = torch.from_numpy(va @ vb.T) + bias.double().cpu()
@@ -218,6 +219,30 @@ def test_matmul8_with_a_split_contraction(m, n, k, dt):
     ctx.matmul8(a, b, out[:, 1:n + 1], bias=bias, beta=1.0)
     assert torch.equal(out[:, 1:n + 1].cpu(), (want + 2).to(dt))
     assert bool((out[:, 0] == 3).all()) and bool((out[:, n + 1] == 3).all())
+
+
+@pytest.mark.parametrize("m,n,k,fmt", [(17, 4096, 4096, "e4m3"), (33, 1030, 4000, "e5m2"), (63, 31, 5100, "e4m3"),
+                                       (64, 2049, 2300, "e5m2"), (133, 333, 5249, "e4m3"), (600, 33, 3100, "e5m2"),
+                                       (33, 9000, 4096, "e4m3"), (20, 33, 1537, "e5m2")])
+@pytest.mark.parametrize("dt", [BF, FP])
+def test_matmul8_few_rows_and_a_long_k(ctx, m, n, k, fmt, dt):
+    """Tiles of 64 x 32 whose four groups of waves share k, some of them with nothing left
+    of it: whole numbers, exactly."""
+    say(f"case: matmul8 few rows {m}x{n}x{k} {fmt} {dt}")
+    a, va = whole_mat(m, m, k, fmt, 1)
+    b, vb = whole_mat(n + 1, n, k, "e4m3", 1)
+    assert np.abs(va).sum(1).max() * np.abs(vb).max() < 2 ** 24
+    want = torch.from_numpy(va @ vb.T)
+    bias = torch.arange(n, dtype=FP).remainder(5).to(dt).cuda()
+    out = torch.full((m + 2, n + 3), 7.0, dtype=dt, device="cuda")
+    mid = out[1:m + 1, 1:n + 1]
+    ctx.matmul8(a, b, mid, bias=bias)
+    assert torch.equal(mid.cpu(), (want + bias.double().cpu()).to(dt))
+    ctx.matmul8(a, b, mid, beta=1.0)
+    again = ((want + bias.double().cpu()).to(dt).double() + want).to(dt)
+    assert torch.equal(mid.cpu(), again)
+    out[1:m + 1, 1:n + 1] = 7
+    assert bool((out == 7).all())
 
 
 @pytest.mark.parametrize("m,n,k,fmt", [(4096, 4096, 500, "e4m3"), (5000, 5000, 2048, "e5m2"), (5000, 5001, 1990, "e4m3"),
