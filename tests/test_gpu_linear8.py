@@ -292,6 +292,38 @@ def test_matmul8_on_quantised_values(ctx, m, n, k, fmt):
     assert torch.equal(out, again)
 
 
+def test_matmul8_without_a_bias_after_one_with(ctx):
+    """Nothing of a call's bias is left on the chip for the next one; a replayed graph of
+    both gives the same."""
+    m, n, k = 5000, 5000, 2048
+    a, va = whole_mat(m, m, k, "e4m3", 0)
+    b, vb = whole_mat(n + 1, n, k, "e4m3", 0)
+    want = torch.from_numpy(va.astype(np.float32) @ vb.astype(np.float32).T)
+    bias = torch.full((n,), 2.0 ** 20, dtype=BF, device="cuda")
+    with_, without = torch.empty(m, n, dtype=BF, device="cuda"), torch.empty(m, n, dtype=BF, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        c = pk.Context(pk.config("tiny"), stream=s)
+
+        def both():
+            c.matmul8(a, b, with_, bias=bias)
+            c.matmul8(a, b, without)
+        both()
+        s.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            both()
+        for i in range(4):
+            if i:
+                with_.fill_(1)
+                without.fill_(1)
+                g.replay()
+            s.synchronize()
+            assert torch.equal(without.cpu(), want.to(BF)), i
+            assert torch.equal(with_.cpu(), (want + 2.0 ** 20).to(BF)), i
+
+
 def test_matmul8_carries_nan_and_zero_blocks(ctx):
     m, n, k = 70, 50, 700
     x, w = rand(1, m, k), rand(2, n, k)
