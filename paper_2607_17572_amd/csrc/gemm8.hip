@@ -13,9 +13,15 @@
 // spread scales the sums are 1e-5 to 3e-5 off (relative, 2-norm, whatever k is), a
 // fiftieth of the rounding to bf16 that follows.
 //
-// fp32 results: the values as bf16 (every 8-bit value with its scale is one:
-// v_cvt_scalef32_pk_bf16_fp8) through v_mfma_f32_32x32x16_bf16, whose sums are fp32,
-// at half the rate.
+// fp32 results: the values as bf16 (v_cvt_scalef32_pk_bf16_fp8) through
+// v_mfma_f32_32x32x16_bf16, whose sums are fp32, at half the rate.  bf16 holds every value
+// of a block whose scale is below 2^113 (E4M3: 2^120), down to multiples of 2^-133.  A
+// wave that met a scale of 2^17 or more drops its sums and starts again with the 8-bit
+// instruction, whose scales have no such limit, eight times for each 64 of k and each time
+// with one of the 8 neighbours only (large_scales, one_of_8): fp32 sums again, and what
+// bf16 rounds off of values below 2^-126 has met no factor of 2^32 or more.  4096 x 4096,
+// k 9216 with large scales everywhere: 976 us instead of 223, of which looking for them
+// takes 2.
 #include <type_traits>
 
 #include "q8.h"
@@ -32,6 +38,18 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // scale byte as the factor it stands for (as the conversion takes it)
 __device__ __forceinline__ float scale_of(int s) { return __uint_as_float(s == 255 ? 0x7fc00000u : (uint32_t)s << 23); }
+
+// Nonzero if one of a word's exponent bytes is 144 .. 254 (a scale of 2^17 or more).
+__device__ __forceinline__ uint32_t large_scales(uint32_t w) {
+  return ((w & 0x70707070u) + 0x70707070u) & ~((w & 0x7f7f7f7fu) + 0x01010101u) & w & 0x80808080u;
+}
+// The p-th of every eight bytes (two words), zeros for the rest.
+__device__ __forceinline__ i32x8 one_of_8(i32x8 v, int p) {
+  const int even = p < 4 ? (int)(0xffu << (8 * p)) : 0, odd = p < 4 ? 0 : (int)(0xffu << (8 * (p - 4)));
+#pragma unroll
+  for (int w = 0; w < 8; ++w) v[w] &= w & 1 ? odd : even;
+  return v;
+}
 
 // eight 8-bit values (two words) times a scale, as bf16
 template <int F>
@@ -325,6 +343,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void matmul8_tile_k(Matmul8Args 
     for (int j = 0; j < FN; ++j) nb[j] = sb[pb[j]];
   };
 
+  uint64_t large = 0;  // lanes that met a scale beyond what bf16 is used for
   i32x8 fa[FM], fb[2][FN];
   bf16x8 xb[EXACT ? FN : 1][4];
   auto mfma_half = [&](int half, int buf) {
@@ -383,6 +402,14 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void matmul8_tile_k(Matmul8Args 
 #pragma unroll
       for (int j = 0; j < FN; ++j) wb[j] = nb[j];
       words(kt0 + kt + 8);
+      if constexpr (EXACT) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) w |= large_scales(wa[i]);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) w |= large_scales(wb[j]);
+        large |= __ballot(w != 0);
+      }
     } else if constexpr (c % 2 == 0) {  // the next block of 128
 #pragma unroll
       for (int i = 0; i < FM; ++i) wa[i] >>= 8;
@@ -435,6 +462,43 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void matmul8_tile_k(Matmul8Args 
     for (int i = nk; i < nkg; ++i) __builtin_amdgcn_s_barrier();
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
+
+  if constexpr (EXACT) {
+    if (large) {  // the wave's products once more, from memory
+      auto chunks = [](const uint8_t* p) {
+        return __builtin_shufflevector(*(const i32x4*)p, *(const i32x4*)(p + 32), 0, 1, 2, 3, 4, 5, 6, 7);
+      };
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+#pragma unroll 1
+      for (int t = kt0; t < kt0 + nk; ++t) {
+        const int at = t * BK + 16 * h, sh = 8 * (t / 2 & 3);
+        const uint32_t *sa = g.a.sc + (size_t)(t / 8) * M, *sb = g.b.sc + (size_t)(t / 8) * N;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+          fb[0][j] = chunks(g.b.q + pb[j] * g.b.ld + at);
+          wb[j] = sb[pb[j]] >> sh;
+        }
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+          const i32x8 a = chunks(g.a.q + pa[i] * g.a.ld + at);
+          wa[i] = sa[pa[i]] >> sh;
+#pragma unroll 1
+          for (int p = 0; p < 8; ++p) {
+            const i32x8 x = one_of_8(a, p);
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+              acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[0][j], x, acc[i][j], 0, FA, 0, (int)wb[j], 0,
+                                                                          (int)wa[i]);
+          }
+        }
+      }
+    }
+  }
 
   auto stn = [&](int i) { return i == 0 ? st0 : i == 1 ? st1 : i == 2 ? st2 : st3; };
   if constexpr (KG > 1) {
@@ -839,6 +903,7 @@ __global__ __launch_bounds__(512) void matmul8_few_k(Matmul8Args g) {
   const uint8_t* const pb = g.b.q + rb * g.b.ld + 16 * q;
   const int sh = 8 * (wave & 3);  // the blocks of a wave have one place in their exponent words
   f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  uint32_t large = 0;
 
   // blocks b0, b0 + KW, ... (UU of them): all loads, then all products
   auto blocks = [&](auto uu, int b0) {
@@ -860,6 +925,7 @@ __global__ __launch_bounds__(512) void matmul8_few_k(Matmul8Args g) {
         acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u], fa[u], acc, 0, FA, 0, (int)(wb[u] >> sh), 0,
                                                                (int)(wa[u] >> sh));
       } else {
+        large |= large_scales((wa[u] >> sh) & 255u) | large_scales((wb[u] >> sh) & 255u);
 #pragma unroll
         for (int w = 0; w < 8; w += 2)
           acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<E4M3>(fb[u][w], fb[u][w + 1], scale_of((wb[u] >> sh) & 255u)),
@@ -871,6 +937,19 @@ __global__ __launch_bounds__(512) void matmul8_few_k(Matmul8Args g) {
   int b0 = wave;
   for (; b0 + KW * (U - 1) < nk; b0 += KW * U) blocks(std::integral_constant<int, U>(), b0);
   for (; b0 < nk; b0 += KW) blocks(std::integral_constant<int, 1>(), b0);
+  if (sizeof(T) == 4 && __ballot(large != 0)) {  // the wave's products once more
+    auto chunks = [](const uint8_t* p) {
+      return __builtin_shufflevector(*(const i32x4*)p, *(const i32x4*)(p + 64), 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (size_t b = wave; b < (size_t)nk; b += KW) {
+      const i32x8 fa = chunks(pa + b * 128), fb = chunks(pb + b * 128);
+      const uint32_t wa = (g.a.sc + b / 4 * M)[ra] >> sh, wb = (g.b.sc + b / 4 * N)[rb] >> sh;
+#pragma unroll 1
+      for (int p = 0; p < 8; ++p)
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb, one_of_8(fa, p), acc, 0, FA, 0, (int)wb, 0, (int)wa);
+    }
+  }
   red[wave][lane] = acc;
   __syncthreads();
   if (wave == 0 && l < M) {

@@ -1,0 +1,169 @@
+"""What the 8-bit product keeps of its operands' range and sums, on the GPU against the
+definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_17572_amd as pk
+from oracle import linear8 as o8
+
+pytestmark = pytest.mark.gpu
+
+BF, FP = torch.bfloat16, torch.float32
+FMT = {"e4m3": pk.E4M3, "e5m2": pk.E5M2}
+
+
+@pytest.fixture(autouse=True)
+def fp32_default():
+    """Another test file sets fp64 as the default type."""
+    was = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(was)
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    return pk.Context(pk.config("tiny"))
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def code(v, fmt):
+    return int(np.nonzero(o8.table8(fmt) == v)[0][0])
+
+
+def rows_of(m, rows):
+    """The given rows of a Mat8 as fp64 values."""
+    q = o8.table8("e5m2" if m.fmt else "e4m3")[m.q[rows].cpu().numpy()]
+    s = m.scale[:, rows].cpu().numpy().transpose(1, 0, 2).reshape(len(rows), -1).astype(np.int64)
+    return o8.values8(q[:, :m.k], s)
+
+
+def single(rows, k, block, fmt, values, scales):
+    """One nonzero value a row, in the given block of 128: (Mat8, fp64 value of each row)."""
+    m = pk.Mat8(rows, k, FMT[fmt])
+    m.q.zero_()
+    m.scale.fill_(127)
+    v = [values[i % len(values)] for i in range(rows)]
+    s = [scales[i // 3 % len(scales)] for i in range(rows)]
+    m.q[:, 128 * block + 5] = torch.tensor([code(x, fmt) for x in v], dtype=torch.uint8, device="cuda")
+    m.scale[block // 4, :, block % 4] = torch.tensor(s, dtype=torch.uint8, device="cuda")
+    return m, np.array(v) * np.ldexp(1.0, np.array(s) - 127)
+
+
+def some(n):
+    """Up to 60 of n indexes, the last ones among them."""
+    return sorted({int(i) for i in np.linspace(0, n - 1, min(n, 55))} | {max(0, n - 1 - i) for i in range(5)})
+
+
+# a single row; 64 x 32 and 64 x 64 tiles, with splits of k; 128 x 128; 256 x 256
+SHAPES = [(1, 150, 700), (13, 40, 2000), (40, 300, 2300), (70, 150, 700), (130, 2000, 700), (40, 300, 9000), (1100, 70, 15000),
+          (2100, 2100, 400), (4096, 4096, 4000)]
+SCALES = [254, 0, 127, 143, 144, 17, 239, 240, 246, 247, 253, 1, 100, 200, 64, 9]
+
+
+@pytest.mark.parametrize("m,n,k", SHAPES)
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("dt", [FP, BF])
+def test_products_of_every_scale(ctx, m, n, k, fmt, dt):
+    """One product an element, of 8 significant bits at most: exact wherever fp32 (bf16:
+    its rounding) holds it, infinite past the largest, within one step of 2^-149 below the
+    normal range (bf16: 2^-133)."""
+    say(f"case: scales {m}x{n}x{k} {fmt} {dt}")
+    top = [57344.0, 2.0 ** -16] if fmt == "e5m2" else [448.0, 2.0 ** -9]
+    last = -(-k // 128) - 1
+    for block in {0, last // 2}:  # (with an odd first block, a split that is not the first, or a group of waves)
+        a, va = single(m, k, block, fmt, [1.0, top[0], -top[1], 1.5, -top[0]], SCALES)
+        b, vb = single(n, k, block, "e4m3", [1.125, -448.0, 2.0 ** -9, 1.0], SCALES[1:] + SCALES[:1] if m > 1 else [254, 100, 247])
+        out = torch.empty(m, n, dtype=dt, device="cuda")
+        ctx.matmul8(a, b, out)
+        i, j = some(m), some(n)
+        got = f64(out[i][:, j])
+        want = f64(torch.from_numpy(np.outer(va[i], vb[j])).to(dt))
+        # a wave of up to 32 rows and columns, or more of them, meets every scale: the values
+        # that bf16 would round below 2^-126 come through too
+        least = 2.0 ** -133 if dt is BF else 2.0 ** -149
+        small = np.abs(np.outer(va[i], vb[j])) < 2.0 ** -126
+        if m == 1:  # row 0 has the largest scale
+            assert va[0] >= 2.0 ** 127
+        assert not np.isnan(got).any()
+        assert np.array_equal(got[~small], want[~small])
+        assert (np.abs(got[small] - want[small]) <= least).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 200, 900), (33, 1030, 1400), (600, 700, 1100)])
+def test_values_below_the_normal_range(ctx, m, n, k):
+    """No scale of 2^17 or more: a value below 2^-126 counts as the nearest multiple of
+    2^-133, so a product is off by at most 2^-134 times the other factor."""
+    say(f"case: small values {m}x{n}x{k}")
+    a, va = single(m, k, 3, "e4m3", [1.0, 448.0, 2.0 ** -9, 1.125 * 2.0 ** -6, -1.75], [0, 1, 2, 3, 9])
+    b, vb = single(n, k, 3, "e4m3", [1.0, -1.375, 448.0], [127, 140, 143])
+    out = torch.empty(m, n, device="cuda")
+    ctx.matmul8(a, b, out)
+    i, j = some(m), some(n)
+    got, want = f64(out[i][:, j]), np.outer(va[i], vb[j])
+    assert (np.abs(got - want) <= 2.0 ** -134 * np.abs(vb[j]) + 2.0 ** -149).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 129, 2200), (40, 300, 2300), (130, 2000, 700), (40, 300, 9000), (2100, 2100, 400)])
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_sums_with_large_scales(ctx, m, n, k, fmt):
+    """Operands of 2^60 and 2^-60: fp32 sums all the same.  Each product of 8 bits is
+    exact; one of the 8 neighbours of k at a time, an instruction adds at most 16 products
+    and what was there, each off by at most 2^-23 of the magnitudes so far: over k / 64 times 8
+    instructions less than 17 k / 8 such steps, and 64 for the joins."""
+    say(f"case: large scales {m}x{n}x{k} {fmt}")
+    g = torch.Generator().manual_seed(m + n)
+    a, b = pk.Mat8(m, k, FMT[fmt]), pk.Mat8(n, k)
+    x = torch.randn(m, k, generator=g) * torch.exp(1.5 * torch.randn(m, k, generator=g))
+    ctx.quantize8((x * 2.0 ** 60).cuda(), a)
+    ctx.quantize8((torch.randn(n, k, generator=g) * 2.0 ** -60).cuda(), b, tile=True)
+    out = torch.empty(m, n, device="cuda")
+    ctx.matmul8(a, b, out)
+    i, j = some(m), some(n)
+    va, vb = rows_of(a, i), rows_of(b, j)
+    bound = (17 * k / 8 + 64) * 2.0 ** -23 * (np.abs(va) @ np.abs(vb).T)
+    assert (np.abs(f64(out[i][:, j]) - va @ vb.T) <= bound).all()
+    # the same data at ordinary scales gives the same sums but for their rounding
+    ctx.quantize8(x.cuda(), a)
+    plain = torch.empty_like(out)
+    ctx.matmul8(a, b, plain)
+    assert (np.abs(f64(out[i][:, j]) - f64(plain[i][:, j]) * 2.0 ** 60) <= 2 * bound).all()
+
+
+def test_the_largest_values_a_quantiser_takes(ctx):
+    """A block at the largest fp32 value rounds up to 2^128 (256 2^120): a product with a
+    small factor is finite."""
+    m, n, k = 37, 90, 300
+    x = torch.randn(m, k)
+    x[3, 200], x[7, 4] = torch.finfo(FP).max, -torch.finfo(FP).max
+    a, b = pk.Mat8(m, k), pk.Mat8(n, k)
+    ctx.quantize8(x.cuda(), a)
+    ctx.quantize8((torch.randn(n, k) * 2.0 ** -20).cuda(), b)
+    out = torch.empty(m, n, device="cuda")
+    ctx.matmul8(a, b, out)
+    va, vb = rows_of(a, range(m)), rows_of(b, range(n))
+    assert va[3, 200] == 2.0 ** 128
+    bound = (17 * k / 8 + 64) * 2.0 ** -23 * (np.abs(va) @ np.abs(vb).T)
+    assert (np.abs(f64(out) - va @ vb.T) <= bound).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 40, 700), (70, 50, 700), (600, 700, 1100), (2100, 2100, 400)])
+def test_nan_beside_large_scales(ctx, m, n, k):
+    """A block of exponent 255 makes its row NaN, a large scale beside it changes nothing."""
+    say(f"case: nan and large {m}x{n}x{k}")
+    a, va = single(m, k, 1, "e4m3", [1.0, -3.0], [127, 200])
+    b, vb = single(n, k, 1, "e4m3", [2.0, 0.5], [127])
+    a.scale[0, 2, 0] = 255
+    out = torch.empty(m, n, device="cuda")
+    ctx.matmul8(a, b, out)
+    assert bool(out[2].isnan().all()) and int(out.isnan().sum()) == n
+    i, j = [r for r in some(m) if r != 2], some(n)
+    assert np.array_equal(f64(out[i][:, j]), np.outer(va[i], vb[j]))
