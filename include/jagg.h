@@ -401,10 +401,15 @@ jagg_status jagg_quantize8(jagg_ctx* ctx, const void* x, size_t ldx, int rows, i
 
 /* out[m][n] = beta * out[m][n] + sum_k a(m, k) b(n, k) + bias[n], in a fixed order.
  * JAGG_F32: fp32 sums, for every scale (2^17 and more: up to five times slower; a value
- * below 2^-126 may count as the nearest multiple of 2^-133).  JAGG_BF16: the 8-bit
- * matrix instructions' sums, which add 8 neighbours of k with 14 bits of the largest
- * and everything else in fp32 (1e-5 to 3e-5 relative to the result's 2-norm, where
- * the rounding to bf16 is 1.7e-3).  a: E4M3 or E5M2, b: E4M3 (EUNSUPPORTED otherwise), of
+ * below 2^-126 may count as the nearest multiple of 2^-133).  JAGG_BF16: the same
+ * sums for few rows and small results; for larger ones, where they would take twice
+ * the time, the 8-bit matrix instructions', which cut the products of 8 neighbours of k
+ * off 13 bits below the exponent of the largest and are fp32 between such groups: an
+ * element is off by less than 2^-10 of each group's largest |a b| (an 8-bit subnormal
+ * counting as the least normal), summed over the groups, before it is rounded to bf16
+ * (measured on normally distributed data: 1e-5 to 3e-5 of the result's 2-norm, where
+ * that rounding is 1.7e-3).  A result whose large terms cancel is better taken in
+ * fp32.  a: E4M3 or E5M2, b: E4M3 (EUNSUPPORTED otherwise), of
  * equal k.  out: a.rows x b.rows, row stride ldo, out_dtype JAGG_F32 or
  * JAGG_BF16; bias: device, b.rows elements of out_dtype, or NULL; beta 0 or 1.
  * A long k over a small result is split: uses jagg_matmul8_bytes bytes of the bound

@@ -4,17 +4,23 @@
 //
 // Two ways through the matrix cores:
 //
-// bf16 results: v_mfma_scale_f32_32x32x64_f8f6f4, 64 of k an instruction; its scale
-// operands take the block exponents as they are stored, so the product needs no
-// arithmetic beside the matrix instructions.  The instruction adds its products in
-// groups of 8 neighbours of k, aligned to the largest of the group: a product loses
-// what lies 13 bits below that one; between the groups the sums are fp32 (found with
-// operands of one large and one small product).  On normally distributed data with
-// spread scales the sums are 1e-5 to 3e-5 off (relative, 2-norm, whatever k is), a
-// fiftieth of the rounding to bf16 that follows.
+// bf16 results of 128 x 128 and 256 x 256 tiles: v_mfma_scale_f32_32x32x64_f8f6f4, 64 of k
+// an instruction; its scale operands take the block exponents as they are stored, so
+// the product needs no arithmetic beside the matrix instructions.  The instruction adds
+// its products in groups of 8 neighbours of k, aligned to the largest exponent of the
+// group: a product loses what lies 13 bits below that one; between the groups the sums
+// are fp32 (found with operands of one large and one small product).  So a sum is off by
+// less than 2^-10 (7 2^-13) of the largest |product| of each group, added over the groups.
+// On normally distributed data with spread scales that is 1e-5 to 3e-5 (relative, 2-norm,
+// whatever k is), a fiftieth of the rounding to bf16 that follows; the fp32 sums below
+// would take twice the time there (9216 x 16384, k 4096: 465 us).
 //
-// fp32 results: the values as bf16 (v_cvt_scalef32_pk_bf16_fp8) through
-// v_mfma_f32_32x32x16_bf16, whose sums are fp32, at half the rate.  bf16 holds every value
+// Everything else: the values as bf16 (v_cvt_scalef32_pk_bf16_fp8) through
+// v_mfma_f32_32x32x16_bf16, whose sums are fp32, at half the rate.  With up to 16 rows and
+// on 64 x 32 and 64 x 64 tiles the matrix instructions take a small part of the time, so
+// bf16 results have these sums as well (us, against the 8-bit instruction's: one row,
+// 16384 x 4096 14.9, 14.5; 37 x 4096, k 12288 20.3, 19.8; 33 x 1024, k 4096 8.9, 8.3; 512 x 1024,
+// k 1024 6.3, 5.7; 1024 x 1024, k 8192 23.8, 20.8).  bf16 holds every value
 // of a block whose scale is below 2^113 (E4M3: 2^120), down to multiples of 2^-133.  A
 // wave that met a scale of 2^17 or more drops its sums and starts again with the 8-bit
 // instruction, whose scales have no such limit, eight times for each 64 of k and each time
@@ -73,9 +79,8 @@ __device__ __forceinline__ bf16x8 widen8(int w0, int w1, float s) {
 // BM x BN tiles, KG groups of WM x WN waves that split the k tiles and add their sums
 // through LDS.  k tiles of 64 bytes pass through four LDS stages, loaded three ahead
 // straight from memory (the layout, swizzle and barriers of the bf16 direct-to-LDS
-// kernel: 64 bytes are 32 of its k and 64 here, and an instruction takes twice the
-// bytes in twice the time, so its balance of loads, LDS reads and matrix
-// instructions carries over).  A fragment is 32 rows x 64 bytes: a lane takes chunks
+// kernel: 64 bytes are 32 of its k and 64 here, so that loads and LDS reads have twice
+// its matrix instructions to hide behind).  A fragment is 32 rows x 64 bytes: a lane takes chunks
 // h and h + 2 of its row (h = lane / 32), the same on both sides, so the order of k
 // inside the instruction differs from memory's and the sum does not.
 //
@@ -277,7 +282,6 @@ __device__ __forceinline__ void epilogue8(const Matmul8Args& g, const f32x16 (&a
 template <int FA, typename T, int BM, int BN, int WM, int WN, int KG>
 __global__ __launch_bounds__(64 * WM * WN * KG) void matmul8_tile_k(Matmul8Args g) {
   take_split(g);
-  constexpr bool EXACT = sizeof(T) == 4;
   constexpr int BK = 64, NW = WM * WN, FM = BM / (32 * WM), FN = BN / (32 * WN), HM = FM / 2;
   static_assert(FM % 2 == 0, "A's fragments go in two halves");
   constexpr int STG = (BM + BN) * BK, SB = BM * BK;
@@ -345,32 +349,23 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void matmul8_tile_k(Matmul8Args 
 
   uint64_t large = 0;  // lanes that met a scale beyond what bf16 is used for
   i32x8 fa[FM], fb[2][FN];
-  bf16x8 xb[EXACT ? FN : 1][4];
+  bf16x8 xb[FN][4];
   auto mfma_half = [&](int half, int buf) {
-    if constexpr (!EXACT) {
+    if (half == 0) {
 #pragma unroll
-      for (int i = half * HM; i < (half + 1) * HM; ++i)
+      for (int j = 0; j < FN; ++j)
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[buf][j], fa[i], acc[i][j], 0, FA, 0, (int)wb[j], 0,
-                                                                      (int)wa[i]);
-    } else {
-      if (half == 0) {
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-#pragma unroll
-          for (int w = 0; w < 4; ++w)
-            xb[j][w] = widen8<E4M3>(fb[buf][j][2 * w], fb[buf][j][2 * w + 1], scale_of(wb[j] & 255u));
-      }
-#pragma unroll
-      for (int i = half * HM; i < (half + 1) * HM; ++i)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const bf16x8 xa = widen8<FA>(fa[i][2 * w], fa[i][2 * w + 1], scale_of(wa[i] & 255u));
-#pragma unroll
-          for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[j][w], xa, acc[i][j], 0, 0, 0);
-        }
+        for (int w = 0; w < 4; ++w)
+          xb[j][w] = widen8<E4M3>(fb[buf][j][2 * w], fb[buf][j][2 * w + 1], scale_of(wb[j] & 255u));
     }
+#pragma unroll
+    for (int i = half * HM; i < (half + 1) * HM; ++i)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const bf16x8 xa = widen8<FA>(fa[i][2 * w], fa[i][2 * w + 1], scale_of(wa[i] & 255u));
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[j][w], xa, acc[i][j], 0, 0, 0);
+      }
   };
 
   constexpr int NL = OpA::NL + OpB::NL;
@@ -402,14 +397,12 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void matmul8_tile_k(Matmul8Args 
 #pragma unroll
       for (int j = 0; j < FN; ++j) wb[j] = nb[j];
       words(kt0 + kt + 8);
-      if constexpr (EXACT) {
-        uint32_t w = 0;
+      uint32_t w = 0;
 #pragma unroll
-        for (int i = 0; i < FM; ++i) w |= large_scales(wa[i]);
+      for (int i = 0; i < FM; ++i) w |= large_scales(wa[i]);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) w |= large_scales(wb[j]);
-        large |= __ballot(w != 0);
-      }
+      for (int j = 0; j < FN; ++j) w |= large_scales(wb[j]);
+      large |= __ballot(w != 0);
     } else if constexpr (c % 2 == 0) {  // the next block of 128
 #pragma unroll
       for (int i = 0; i < FM; ++i) wa[i] >>= 8;
@@ -463,38 +456,36 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void matmul8_tile_k(Matmul8Args 
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
 
-  if constexpr (EXACT) {
-    if (large) {  // the wave's products once more, from memory
-      auto chunks = [](const uint8_t* p) {
-        return __builtin_shufflevector(*(const i32x4*)p, *(const i32x4*)(p + 32), 0, 1, 2, 3, 4, 5, 6, 7);
-      };
+  if (large) {  // the wave's products once more, from memory
+    auto chunks = [](const uint8_t* p) {
+      return __builtin_shufflevector(*(const i32x4*)p, *(const i32x4*)(p + 32), 0, 1, 2, 3, 4, 5, 6, 7);
+    };
 #pragma unroll
-      for (int i = 0; i < FM; ++i)
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
+      for (int j = 0; j < FN; ++j)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 #pragma unroll 1
-      for (int t = kt0; t < kt0 + nk; ++t) {
-        const int at = t * BK + 16 * h, sh = 8 * (t / 2 & 3);
-        const uint32_t *sa = g.a.sc + (size_t)(t / 8) * M, *sb = g.b.sc + (size_t)(t / 8) * N;
+    for (int t = kt0; t < kt0 + nk; ++t) {
+      const int at = t * BK + 16 * h, sh = 8 * (t / 2 & 3);
+      const uint32_t *sa = g.a.sc + (size_t)(t / 8) * M, *sb = g.b.sc + (size_t)(t / 8) * N;
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          fb[0][j] = chunks(g.b.q + pb[j] * g.b.ld + at);
-          wb[j] = sb[pb[j]] >> sh;
-        }
+      for (int j = 0; j < FN; ++j) {
+        fb[0][j] = chunks(g.b.q + pb[j] * g.b.ld + at);
+        wb[j] = sb[pb[j]] >> sh;
+      }
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-          const i32x8 a = chunks(g.a.q + pa[i] * g.a.ld + at);
-          wa[i] = sa[pa[i]] >> sh;
+      for (int i = 0; i < FM; ++i) {
+        const i32x8 a = chunks(g.a.q + pa[i] * g.a.ld + at);
+        wa[i] = sa[pa[i]] >> sh;
 #pragma unroll 1
-          for (int p = 0; p < 8; ++p) {
-            const i32x8 x = one_of_8(a, p);
+        for (int p = 0; p < 8; ++p) {
+          const i32x8 x = one_of_8(a, p);
 #pragma unroll
-            for (int j = 0; j < FN; ++j)
-              acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[0][j], x, acc[i][j], 0, FA, 0, (int)wb[j], 0,
-                                                                          (int)wa[i]);
-          }
+          for (int j = 0; j < FN; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[0][j], x, acc[i][j], 0, FA, 0, (int)wb[j], 0,
+                                                                        (int)wa[i]);
         }
       }
     }
@@ -921,23 +912,18 @@ __global__ __launch_bounds__(512) void matmul8_few_k(Matmul8Args g) {
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int u = 0; u < UU; ++u) {
-      if constexpr (sizeof(T) == 2) {
-        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u], fa[u], acc, 0, FA, 0, (int)(wb[u] >> sh), 0,
-                                                               (int)(wa[u] >> sh));
-      } else {
-        large |= large_scales((wa[u] >> sh) & 255u) | large_scales((wb[u] >> sh) & 255u);
+      large |= large_scales((wa[u] >> sh) & 255u) | large_scales((wb[u] >> sh) & 255u);
 #pragma unroll
-        for (int w = 0; w < 8; w += 2)
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<E4M3>(fb[u][w], fb[u][w + 1], scale_of((wb[u] >> sh) & 255u)),
-                                                        widen8<FA>(fa[u][w], fa[u][w + 1], scale_of((wa[u] >> sh) & 255u)), acc,
-                                                        0, 0, 0);
-      }
+      for (int w = 0; w < 8; w += 2)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<E4M3>(fb[u][w], fb[u][w + 1], scale_of((wb[u] >> sh) & 255u)),
+                                                      widen8<FA>(fa[u][w], fa[u][w + 1], scale_of((wa[u] >> sh) & 255u)), acc, 0,
+                                                      0, 0);
     }
   };
   int b0 = wave;
   for (; b0 + KW * (U - 1) < nk; b0 += KW * U) blocks(std::integral_constant<int, U>(), b0);
   for (; b0 < nk; b0 += KW) blocks(std::integral_constant<int, 1>(), b0);
-  if (sizeof(T) == 4 && __ballot(large != 0)) {  // the wave's products once more
+  if (__ballot(large != 0)) {  // the wave's products once more
     auto chunks = [](const uint8_t* p) {
       return __builtin_shufflevector(*(const i32x4*)p, *(const i32x4*)(p + 64), 0, 1, 2, 3, 4, 5, 6, 7);
     };
@@ -1012,17 +998,17 @@ enum Kind8 { K8_FEW, K8_32, K8_64, K8_128, K8_256 };
 // Tiles and splits of k: the least estimated time (us) = rounds of the 256 CUs x (blocks
 // of 128 of a split x time per block + prologue and epilogue), and for a split the
 // second launch and the sums' way through memory.  The times per block are those
-// measured with every CU busy: bf16 0.25 (64 x 64), 0.58 (128 x 128; 1.0 for two on a
-// CU), 1.4 (256 x 256); fp32 0.29, 0.78 (1.65), 3.2.  64 x 32 tiles, each of four groups of
-// waves with a quarter of k, need no second launch but read the left operand twice as
-// often: 0.42 per block of a group on up to 32 CUs, 0.5 (17 rows) to 0.78 (64) above, 1 in
-// more than one round.  Over 320 sizes drawn from 17 .. 9000 rows, 64 .. 16384 columns and k
-// the choice takes 0.99 times the best of four tiles x eight splits in the mean and 1.22
-// times at most.  Examples (us, bf16; 64 x 32, 64 x 64 in one and four splits, 128 x 128):
-// 37 x 4096, k 12288: 21, 32, 16, 78; 18 x 7040, k 4864: 9.9, 12, 13, 20; 31 x 326, k 5248: 7.6,
-// 9.3, 10, 17; 1024 x 4096, k 4096: -, 37, 64, 20; 8192 x 8192, k 512: 128 x 128 79, 256 x 256
-// 62; 6144 x 6144, k 1024: 50, 52.  The single-token kernel up to 16 rows: 13.8 at 16 x 4096,
-// k 12288 (64 x 64 tiles in four splits: 15.0).
+// measured with every CU busy: 0.29 (64 x 64); bf16 0.58 (128 x 128; 1.0 for two on a CU), 1.4
+// (256 x 256); fp32 0.78 (1.65), 3.2.  64 x 32 tiles, each of four groups of waves with a
+// quarter of k, need no second launch but read the left operand twice as often: 0.53 per
+// block of a group on up to 32 CUs, 0.63 (17 rows) to 0.98 (64) above, 1.25 in more than one
+// round.  Over 110 sizes drawn from 17 .. 9000 rows, 64 .. 16384 columns and k the choice takes
+// 0.99 times the best of four tiles x eight splits in the mean and 1.19 times at most.
+// Examples (us, bf16; 64 x 32, 64 x 64 in one and four splits, 128 x 128): 37 x 4096, k 12288:
+// 21.5, 28.5, 16.6, 42.7; 18 x 7040, k 4864: 11.1, 14.1, 16.2, 19.5; 31 x 326, k 5248: 10.4, 15.8,
+// 12.1, 16.6; 1024 x 4096, k 4096: 78, 47, 73, 21; 8192 x 8192, k 512: 128 x 128 80, 256 x 256 64;
+// 6144 x 6144, k 1024: 51.8, 54.2.  The single-token kernel up to 16 rows: 14.3 at 16 x 4096,
+// k 12288 (64 x 64 tiles in four splits with 17 rows: 15.7).
 
 size_t matmul8_plan(Matmul8Args& g) {
   const int M = g.a.rows, N = g.b.rows, nb = (int)(((long)g.a.k + 127) / 128);
@@ -1043,10 +1029,10 @@ size_t matmul8_plan(Matmul8Args& g) {
       double t;
       if (kind == K8_32) {
         if (s > 1) break;  // its four groups of k are the split
-        const double one = wgs > 256 ? 1.0 : wgs > 32 ? 0.5 + 0.006 * ((M < 64 ? M : 64) - 17) : 0.42;
-        t = 2.8 + (wgs + 255) / 256 * ((nb + 15) / 16 * 4 * (f32 ? 1.25 : 1.0) * one);
+        const double one = wgs > 256 ? 1.25 : wgs > 32 ? 0.625 + 0.0075 * ((M < 64 ? M : 64) - 17) : 0.525;
+        t = 2.8 + (wgs + 255) / 256 * ((nb + 15) / 16 * 4 * one);
       } else if (kind == K8_64) {
-        t = 2.0 + (wgs + 255) / 256 * (ps * (f32 ? 0.29 : 0.25) + 1.5);
+        t = 2.0 + (wgs + 255) / 256 * (ps * 0.29 + 1.5);
       } else if (kind == K8_128) {  // two workgroups per CU
         const double one = ps * (f32 ? 0.78 : 0.58) + 2.5, two = ps * (f32 ? 1.65 : 1.0) + 3.5;
         const long rest = wgs % 512;

@@ -167,3 +167,77 @@ def test_nan_beside_large_scales(ctx, m, n, k):
     assert bool(out[2].isnan().all()) and int(out.isnan().sum()) == n
     i, j = [r for r in some(m) if r != 2], some(n)
     assert np.array_equal(f64(out[i][:, j]), np.outer(va[i], vb[j]))
+
+
+def operands(ctx, m, n, k, fmt, cancel):
+    """Quantised random operands.  cancel: some of k's columns are 100 times larger on the
+    left and meet their negatives `cancel` columns later, with the same weights: they add
+    up to nothing, in the same group of 8 neighbours (1) or in the next one (8)."""
+    g = torch.Generator(device="cuda").manual_seed(m + n + k + cancel)
+    x = torch.randn(m, k, generator=g, device="cuda")
+    w = torch.randn(n, k, generator=g, device="cuda")
+    if cancel:
+        at = torch.arange(3, k - 16, 48, device="cuda")
+        at = at[at % 128 < 112]
+        x[:, at] *= 100
+        x[:, at + cancel] = -x[:, at]
+        w[:, at + cancel] = w[:, at]
+    a, b = pk.Mat8(m, k, FMT[fmt]), pk.Mat8(n, k)
+    ctx.quantize8(x, a)
+    ctx.quantize8(w, b)
+    return a, b
+
+
+def magnitude(v, m, rows):
+    """|values|, a subnormal 8-bit value counting as the least normal one."""
+    s = m.scale[:, rows].cpu().numpy().transpose(1, 0, 2).reshape(len(rows), -1).astype(np.int64)
+    least = np.repeat(np.ldexp(1.0, s - 127 - (14 if m.fmt else 6)), 128, axis=1)[:, :m.k]
+    return np.where(v == 0, 0.0, np.maximum(np.abs(v), least))
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 700, 4100), (5, 129, 2200), (40, 300, 2300), (130, 2000, 700), (40, 300, 9000), (256, 256, 16000)])
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("cancel", [0, 1, 8])
+def test_bf16_results_of_small_products(ctx, m, n, k, fmt, cancel):
+    """fp32 sums, whatever cancels: each of at most 64 additions inside an instruction and
+    of k / 64 + 64 between them is off by at most 2^-23 of the sum of magnitudes so far; one
+    rounding to bf16."""
+    say(f"case: bf16 result {m}x{n}x{k} {fmt} cancel={cancel}")
+    a, b = operands(ctx, m, n, k, fmt, cancel)
+    out = torch.empty(m, n, dtype=BF, device="cuda")
+    ctx.matmul8(a, b, out)
+    i, j = some(m), some(n)
+    va, vb = rows_of(a, i), rows_of(b, j)
+    want, size = va @ vb.T, np.abs(va) @ np.abs(vb).T
+    bound = (k / 64 + 128) * 2.0 ** -23 * size
+    err = np.abs(f64(out[i][:, j]) - want)
+    assert (err <= bound + 2.0 ** -8 * (np.abs(want) + bound)).all()
+
+
+# 128 x 128 tiles, with splits of k; 256 x 256, and from tile to tile
+@pytest.mark.parametrize("m,n,k", [(2100, 2100, 400), (1000, 2000, 9000), (5000, 5001, 1990), (5000, 5000, 2048)])
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("cancel", [0, 1, 8])
+def test_bf16_results_of_large_products(ctx, m, n, k, fmt, cancel):
+    """The 8-bit instructions' sums: of 8 neighbours of k, the products are cut off 13 bits
+    below the exponent of the largest, so the other seven lose less than 2^-13 of it
+    each; between the groups, 9 additions for each 64 of k and 64 for the joins, off by at
+    most 2^-23 of the magnitudes; one rounding to bf16."""
+    say(f"case: bf16 result {m}x{n}x{k} {fmt} cancel={cancel}")
+    a, b = operands(ctx, m, n, k, fmt, cancel)
+    out = torch.empty(m, n, dtype=BF, device="cuda")
+    ctx.matmul8(a, b, out)
+    i, j = some(m), some(n)
+    va, vb = rows_of(a, i), rows_of(b, j)
+    want, size = va @ vb.T, np.abs(va) @ np.abs(vb).T
+    pad = -k % 8
+    ma, mb = (np.pad(magnitude(v, x, r), ((0, 0), (0, pad))) for v, x, r in ((va, a, i), (vb, b, j)))
+    group = np.zeros_like(want)
+    for c in range(0, k + pad, 8):
+        group += (ma[:, None, c:c + 8] * mb[None, :, c:c + 8]).max(2)
+    bound = 7 * 2.0 ** -13 * group + (9 * k / 64 + 64) * 2.0 ** -23 * size
+    err = np.abs(f64(out[i][:, j]) - want)
+    assert (err <= bound + 2.0 ** -8 * (np.abs(want) + bound)).all()
+    if not cancel:  # on normally distributed data the sums come close to fp32's
+        rel = np.linalg.norm(f64(out[i][:, j]) - want) / np.linalg.norm(want)
+        assert rel <= 2.0 ** -9
