@@ -145,15 +145,18 @@ def _handle(pk, m, k, fmt):
     return pk.Mat8(m["rows"], k, fmt=pk.E5M2 if fmt == "e5m2" else pk.E4M3, q=m["q"], scale=m["scale"])
 
 
-_kept = []
+_kept = {}
 
 
 def _context():
-    """The program's context: one for all calls, as a training program keeps it."""
+    """The program's context: one for all calls on the current stream, to which it is
+    bound, as a training program keeps it."""
     import paper_2607_17572_amd as pk
-    if not _kept:
-        _kept.append(pk.Context(pk.config("tiny")))
-    return pk, _kept[0]
+    device = torch.cuda.current_device()
+    key = device, torch._C._cuda_getCurrentRawStream(device)  # (a Stream object of it takes 3 us to make)
+    if key not in _kept:
+        _kept[key] = pk.Context(pk.config("tiny"))
+    return pk, _kept[key]
 
 
 def prepare(case, seed):
