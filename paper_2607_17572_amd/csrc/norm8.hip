@@ -97,8 +97,9 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm8_k(Norm8Args a) {
     const uint32_t s = exp_byte<E4M3>(max16(m));
     const float k = inv_scale(s);
     if (c < kp) {
-      *(uint2*)(q + c) = make_uint2(pack4<E4M3>(g[0] * k, g[1] * k, g[2] * k, g[3] * k),
-                                    pack4<E4M3>(g[4] * k, g[5] * k, g[6] * k, g[7] * k));
+      *(uint2*)(q + c) = first_bytes(make_uint2(pack4<E4M3>(g[0] * k, g[1] * k, g[2] * k, g[3] * k),
+                                                pack4<E4M3>(g[4] * k, g[5] * k, g[6] * k, g[7] * k)),
+                                     a.cols - c);
     }
     // the wave's four blocks, one word (blocks past the end hold zeros: byte 0)
     const uint32_t w = (uint32_t)__shfl((int)s, 0, 64) | (uint32_t)__shfl((int)s, 16, 64) << 8 |

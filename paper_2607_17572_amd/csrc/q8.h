@@ -76,6 +76,14 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
   return (uint32_t)r;
 }
 
+// the first n of eight bytes, zeros for the rest: padding is zero bytes, whatever the
+// factors and the scale (0 times a negative factor is -0, 0 times NaN NaN)
+__device__ __forceinline__ uint2 first_bytes(uint2 w, int n) {
+  if (n >= 8) return w;
+  const uint64_t m = n > 0 ? ~0ull >> (64 - 8 * n) : 0;
+  return make_uint2(w.x & (uint32_t)m, w.y & (uint32_t)(m >> 32));
+}
+
 __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
 // largest over the 16 lanes of a row of 16
 __device__ __forceinline__ uint32_t max16(uint32_t v) {

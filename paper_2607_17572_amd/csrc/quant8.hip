@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256) void quant8_k(Quant8Args a) {
       const uint2 w = make_uint2(pack4<F>(v[p][0] * k, v[p][1] * k, v[p][2] * k, v[p][3] * k),
                                  pack4<F>(v[p][4] * k, v[p][5] * k, v[p][6] * k, v[p][7] * k));
       if (r0 + p < a.rows) {
-        *(uint2*)(a.out.q + (size_t)(r0 + p) * a.out.ld + c0) = w;
+        *(uint2*)(a.out.q + (size_t)(r0 + p) * a.out.ld + c0) = first_bytes(w, a.cols - c0);
         if (cg == 0) {
           uint8_t* b = sc + ((size_t)(tc >> 2) * a.rows + r0 + p) * 4 + (tc & 3);
           *b = (uint8_t)s;
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(256) void quant8_k(Quant8Args a) {
       const float k = inv_scale(s[e]);
       const uint2 w = make_uint2(pack4<F>(v[0][e] * k, v[1][e] * k, v[2][e] * k, v[3][e] * k),
                                  pack4<F>(v[4][e] * k, v[5][e] * k, v[6][e] * k, v[7][e] * k));
-      *(uint2*)(tr + (cg * 8 + e) * TS + rg * 8) = w;
+      *(uint2*)(tr + (cg * 8 + e) * TS + rg * 8) = first_bytes(w, a.rows - r0);
       if (rg == 0 && c0 + e < a.cols) {
         uint8_t* b = sc + ((size_t)(tr_i >> 2) * a.cols + c0 + e) * 4 + (tr_i & 3);
         *b = (uint8_t)s[e];
