@@ -148,20 +148,21 @@ def _handle(pk, m, k, fmt):
 _kept = {}
 
 
-def _context():
-    """The program's context: one for all calls on the current stream, to which it is
-    bound, as a training program keeps it."""
-    import paper_2607_17572_amd as pk
-    device = torch.cuda.current_device()
+def _context(device=None):
+    """The package and the program's context: one for all calls on the current stream, to
+    which it is bound, as a training program keeps it."""
+    if device is None:
+        device = torch.cuda.current_device()
     key = device, torch._C._cuda_getCurrentRawStream(device)  # (a Stream object of it takes 3 us to make)
     if key not in _kept:
-        _kept[key] = pk.Context(pk.config("tiny"))
-    return pk, _kept[key]
+        import paper_2607_17572_amd as pk
+        _kept[key] = pk, pk.Context(pk.config("tiny"), stream=torch.cuda.current_stream(device))
+    return _kept[key]
 
 
 def prepare(case, seed):
     g, kind = _gen(seed), case["kind"]
-    s = {"case": case}
+    s = {"case": case, "device": torch.cuda.current_device()}
     if kind == "clip":
         lay, n = _layout(case)
         flat = torch.zeros(n, dtype=DT[case["dtype"]], device="cuda")
@@ -299,7 +300,7 @@ def _out8(m):
 
 
 def _kernels(s):
-    pk, ctx = _context()
+    pk, ctx = _context(s["device"])
     case, kind = s["case"], s["case"]["kind"]
     if kind == "clip":
         ctx.clip_grads(s["grads"], case["max_norm"], s["out"], dst=s["parts"], ord=float(case["ord"]))
