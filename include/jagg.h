@@ -460,7 +460,8 @@ jagg_status jagg_grad_norm(jagg_ctx* ctx, const jagg_grad* g, int count, int ord
 
 /* Gradient clipping: out[0] = norm as above, out[1] = c = max_norm / norm if
  * norm > max_norm and 1 otherwise (device, two doubles), then dst = g c for
- * every tensor, in fp32 with one rounding.  A norm that is infinite or NaN
+ * every tensor: c rounded to fp32, the product to fp32, and that to a bf16 dst (a c
+ * below 2^-126 is not rounded: one product in fp64).  A norm that is infinite or NaN
  * gives c = 1: the gradients stay as they are and out[0] tells (the step is the
  * caller's to skip).  dst: host array like g with the same sizes, each of either
  * dtype, or NULL: in place (nothing is written where c = 1).  The tensors of a
