@@ -454,8 +454,10 @@ typedef enum { JAGG_NORM_L2 = 0, JAGG_NORM_MAX = 1 } jagg_norm;
 
 /* norm (device, one double) = sqrt of the sum of squares, or the largest
  * magnitude, of all elements of the list (host array), in fp64; NaN where an
- * element is NaN.  Uses the head of the bound workspace; enqueued on the
- * context's stream, does not synchronise; fixed order. */
+ * element is NaN.  Uses jagg_grad_norm_bytes bytes of the bound workspace;
+ * enqueued on the context's stream, does not synchronise; fixed order (neighbours
+ * in memory count as one tensor). */
+jagg_status jagg_grad_norm_bytes(size_t* bytes);
 jagg_status jagg_grad_norm(jagg_ctx* ctx, const jagg_grad* g, int count, int ord, double* norm);
 
 /* Gradient clipping: out[0] = norm as above, out[1] = c = max_norm / norm if
@@ -466,7 +468,7 @@ jagg_status jagg_grad_norm(jagg_ctx* ctx, const jagg_grad* g, int count, int ord
  * caller's to skip).  dst: host array like g with the same sizes, each of either
  * dtype, or NULL: in place (nothing is written where c = 1).  The tensors of a
  * list must not overlap, nor a dst another tensor; a dst may be its own g.
- * max_norm >= 0. */
+ * max_norm >= 0.  Workspace as jagg_grad_norm. */
 jagg_status jagg_grad_clip(jagg_ctx* ctx, const jagg_grad* g, const jagg_grad* dst, int count, int ord, double max_norm,
                            double* out);
 

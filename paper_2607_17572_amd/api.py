@@ -7,6 +7,7 @@ built, every entry point raises instead of falling back to anything else.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import asdict, dataclass
 
@@ -90,6 +91,7 @@ def lib() -> ctypes.CDLL:
             "jagg_rmsnorm8": [vp, vp, sz, vp, sz, vp, i, i, i, f, vp, sz, pm8, vp],
             "jagg_rmsnorm8_grad_bytes": [i, i, ctypes.POINTER(sz)],
             "jagg_rmsnorm8_grad": [vp, vp, sz, vp, sz, vp, vp, vp, sz, i, i, i, vp, sz, vp, i, f],
+            "jagg_grad_norm_bytes": [ctypes.POINTER(sz)],
             "jagg_grad_norm": [vp, pg, i, i, vp],
             "jagg_grad_clip": [vp, pg, pg, i, i, d, vp],
             "jagg_grpo_composites": [vp, ctypes.POINTER(_GrpoWindow), i, vp, vp, vp],
@@ -298,6 +300,14 @@ class GradList:
 
 def _grads(g) -> GradList:
     return g if isinstance(g, GradList) else GradList([g] if _torch().is_tensor(g) else g)
+
+
+@functools.cache
+def _grad_bytes() -> int:
+    """Workspace of the norm and clipping calls."""
+    n = ctypes.c_size_t()
+    _check(lib().jagg_grad_norm_bytes(ctypes.byref(n)))
+    return n.value
 
 
 _NORMS = {2: 0, 2.0: 0, float("inf"): 1}
@@ -600,7 +610,7 @@ class Context:
         if g.device != self.device or ord not in _NORMS:
             _refuse("the gradients must be on the context's device, ord 2 or inf")
         p = _vec(out, "out", 1, _torch().float64, self.device)
-        self.ensure_workspace(1)
+        self._ensure_bytes(_grad_bytes())
         _check(lib().jagg_grad_norm(self._h, g._c, len(g.tensors), _NORMS[ord], p))
         return out
 
@@ -621,7 +631,7 @@ class Context:
             if not (apart or d is g):
                 self._check_dst(g, d)
         p = _vec(out, "out", 2, _torch().float64, self.device)
-        self.ensure_workspace(1)
+        self._ensure_bytes(_grad_bytes())
         _check(lib().jagg_grad_clip(self._h, g._c, None if d is None else d._c, len(g.tensors), _NORMS[ord],
                                     float(max_norm), p))
         return out

@@ -1333,6 +1333,12 @@ jagg_status grad_list_check(const jagg_ctx* ctx, const jagg_grad* g, const jagg_
     }
   return JAGG_OK;
 }
+constexpr size_t GRAD_WS = jg::GRAD_PART * sizeof(double);
+jagg_status grad_ws_check(const jagg_ctx* ctx, const char* f) {
+  if (ctx->ws && ctx->ws_bytes >= GRAD_WS) return JAGG_OK;
+  return fail(JAGG_EINVAL, std::string(f) + ": workspace not bound or smaller than jagg_grad_norm_bytes = " +
+                               std::to_string(GRAD_WS));
+}
 struct GradLists { const jagg_grad *src, *dst; };
 jg::GradSeg grad_at(const void* list, int i) {
   const GradLists* l = (const GradLists*)list;
@@ -1484,14 +1490,19 @@ jagg_status jagg_rmsnorm8_grad(jagg_ctx* ctx, const void* dy, size_t lddy, const
   return to_status(jg::rmsnorm8_grad(a, ctx->stream));
 }
 
+jagg_status jagg_grad_norm_bytes(size_t* bytes) {
+  if (!bytes) return fail(JAGG_EINVAL, "jagg_grad_norm_bytes: null argument");
+  *bytes = GRAD_WS;
+  return JAGG_OK;
+}
+
 jagg_status jagg_grad_norm(jagg_ctx* ctx, const jagg_grad* g, int count, int ord, double* norm) {
   const char* f = "jagg_grad_norm";
   if (jagg_status st = grad_list_check(ctx, g, nullptr, count, ord, norm, f)) return st;
-  jg::Ws W0;
-  if (jagg_status st = need_head_ws(ctx, W0, f)) return st;
+  if (jagg_status st = grad_ws_check(ctx, f)) return st;
   const GradLists l{g, nullptr};
   OnDevice dev(ctx);
-  return to_status(jg::grad_norm(grad_at, &l, count, ord == JAGG_NORM_MAX, W0.spart, norm, ctx->stream));
+  return to_status(jg::grad_norm(grad_at, &l, count, ord == JAGG_NORM_MAX, (double*)ctx->ws, norm, ctx->stream));
 }
 
 jagg_status jagg_grad_clip(jagg_ctx* ctx, const jagg_grad* g, const jagg_grad* dst, int count, int ord, double max_norm,
@@ -1500,11 +1511,11 @@ jagg_status jagg_grad_clip(jagg_ctx* ctx, const jagg_grad* g, const jagg_grad* d
   if (jagg_status st = grad_list_check(ctx, g, dst, count, ord, out, f)) return st;
   if (!(max_norm >= 0.0) || std::isinf(max_norm))
     return fail(JAGG_EINVAL, std::string(f) + ": max_norm must be >= 0 and finite");
-  jg::Ws W0;
-  if (jagg_status st = need_head_ws(ctx, W0, f)) return st;
+  if (jagg_status st = grad_ws_check(ctx, f)) return st;
   const GradLists l{g, dst ? dst : g};
   OnDevice dev(ctx);
-  return to_status(jg::grad_clip(grad_at, &l, count, ord == JAGG_NORM_MAX, max_norm, W0.spart, out, ctx->stream));
+  return to_status(
+      jg::grad_clip(grad_at, &l, count, ord == JAGG_NORM_MAX, max_norm, (double*)ctx->ws, out, ctx->stream));
 }
 
 jagg_status jagg_group_backward(jagg_ctx* ctx, const void* theta, const void* saved_pair, int batch,
