@@ -328,7 +328,7 @@ class Context:
         self._h = h
         self._ws = None
         self._ws_batch = self._ws_bytes = 0
-        self._in_graph, self._ws_of_graphs = False, []
+        self._captured, self._ws_of_graphs = False, []
         self.layout, self.n_params = param_layout(cfg)
 
     def __del__(self):
@@ -365,20 +365,21 @@ class Context:
         self._ws_batch = batch
 
     def _ensure_bytes(self, nb: int):
-        """A bound workspace of at least nb bytes (it only grows)."""
+        """A bound workspace of at least nb bytes (it only grows).  One that a captured call
+        used stays for as long as the context, since the graph may hold its address."""
         torch = _torch()
-        if torch.cuda.is_current_stream_capturing():
-            self._in_graph = True
+        capturing = torch.cuda.is_current_stream_capturing()
         if self._ws is not None and self._ws_bytes >= nb:
+            self._captured |= capturing
             return
-        if self._in_graph:  # a captured graph may hold the workspace's address: it stays
+        if self._captured:
             self._ws_of_graphs.append(self._ws)
         with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
             ws = torch.empty(nb + 256, dtype=torch.uint8, device=self.device)
         base = ws.data_ptr()
         off = (-base) % 256
         _check(lib().jagg_ctx_set_workspace(self._h, ctypes.c_void_p(base + off), nb))
-        self._ws, self._ws_bytes = ws, nb
+        self._ws, self._ws_bytes, self._captured = ws, nb, capturing
 
     def new_saved(self, batch: int):
         torch = _torch()

@@ -41,3 +41,37 @@ def test_clipping_binds_no_models_workspace():
         ctx.clip_grads([big, t], 1.0, out, dst=[torch.empty_like(big), torch.empty_like(t)], ord=o)
         assert float(out[0]) == (5300000 ** 0.5 if o == 2 else 1.0)
     assert bool((full[:4096] == 0xA5).all()) and bool((full[-4096:] == 0xA5).all())
+
+
+def test_only_a_captured_workspace_outlives_its_successor():
+    """A graph's workspace stays when a larger one is bound; those before and after it,
+    which no graph holds, are freed."""
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        ctx = pk.Context(pk.config("tiny"), stream=s)
+        t, out = torch.full((1000,), 2.0, device="cuda"), torch.empty(2, dtype=DB, device="cuda")
+        dst = torch.empty_like(t)
+        ctx._ensure_bytes(1 << 16)
+        ctx._ensure_bytes(1 << 20)
+        ctx.clip_grads([t], 1.0, out, dst=[dst])
+        s.synchronize()
+        want = dst.clone()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            ctx.clip_grads([t], 1.0, out, dst=[dst])
+        held = ctx._ws
+        was = torch.cuda.memory_allocated()
+        for mb in (64, 128, 256):
+            ctx._ensure_bytes(mb << 20)
+            ctx.clip_grads([t], 1.0, out, dst=[dst])  # eager use in between
+        assert ctx._ws_of_graphs == [held]
+        assert torch.cuda.memory_allocated() - was <= (256 << 20) + (1 << 21)
+        for _ in range(3):
+            dst.zero_()
+            g.replay()
+            s.synchronize()
+            assert torch.equal(dst, want)
+        with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=s):
+            ctx.clip_grads([t], 1.0, out, dst=[dst])
+        ctx._ensure_bytes(300 << 20)
+        assert len(ctx._ws_of_graphs) == 2
