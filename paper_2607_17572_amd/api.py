@@ -254,7 +254,8 @@ def _rows(t, name: str, rows: int, cols: int, dtype, device):
 class Mat8:
     """An 8-bit matrix with one power-of-two scale per block of 128 columns
     (jagg_mat8): ``q`` uint8 [rows][ld], ``scale`` uint8 [ceil(k/512)][rows][4].
-    Allocates both on the current CUDA device, or takes given tensors."""
+    Allocates both on the current CUDA device, or takes given tensors, and keeps
+    them; a call refuses a matrix whose memory is no longer where it was."""
 
     def __init__(self, rows: int, k: int, fmt: int = E4M3, q=None, scale=None):
         torch = _torch()
@@ -276,14 +277,32 @@ class Mat8:
         self.rows, self.k, self.fmt = rows, k, fmt
         self.q, self.scale = q.view(torch.uint8), scale.view(torch.uint8)
         self.device = q.device
-        self._c = _Mat8(q.data_ptr(), scale.data_ptr(), q.shape[1], rows, k, fmt)
+        self._at = self.q.data_ptr(), self.scale.data_ptr()
+        self._c = _Mat8(*self._at, q.shape[1], rows, k, fmt)
+
+    def _arg(self, device):
+        """The C struct for a call on the given device."""
+        if self.device != device:
+            _refuse("an 8-bit matrix must be on the context's device")
+        if (self.q.data_ptr(), self.scale.data_ptr()) != self._at:
+            _refuse("the tensors of an 8-bit matrix have moved since it was made")
+        return self._c
 
 
 class GradList:
     """Gradient tensors (each contiguous, bf16 or fp32, of one GPU) as the norm and
-    clipping calls take them; a program that keeps its gradients keeps one."""
+    clipping calls take them; a program that keeps its gradients keeps one.  The list
+    stands for the memory that the tensors have when it is made, and keeps it: a
+    gradient that is made anew, or a tensor given other memory (``set_``, ``.data``),
+    needs a new list.  A call refuses a list whose memory itself was moved
+    (``resize_`` beyond it)."""
 
     def __init__(self, tensors):
+        self._fill(tensors)
+        held = {s.data_ptr(): s for s in (t.untyped_storage() for t in self.tensors)}
+        self._held = [(s, p) for p, s in held.items()]
+
+    def _fill(self, tensors):
         self.tensors = list(tensors)
         if not self.tensors:
             _refuse("a gradient list needs a tensor")
@@ -297,9 +316,20 @@ class GradList:
         if any(a[1] > b[0] for a, b in zip(self.spans, self.spans[1:])):
             _refuse("gradients must not overlap")
 
+    def _arg(self):
+        for s, p in self._held:
+            if s.data_ptr() != p:
+                _refuse("the memory of a gradient list has moved since it was made")
+        return self._c
+
 
 def _grads(g) -> GradList:
-    return g if isinstance(g, GradList) else GradList([g] if _torch().is_tensor(g) else g)
+    if isinstance(g, GradList):
+        return g
+    one = GradList.__new__(GradList)  # for this call only: the caller holds the memory
+    one._fill([g] if _torch().is_tensor(g) else g)
+    one._held = ()
+    return one
 
 
 @functools.cache
@@ -545,28 +575,25 @@ class Context:
         rows, cols = x.shape
         dt = _dtype_of(x, "x")
         p, ld = _rows(x, "x", rows, cols, x.dtype, self.device)
-        for m in (out, out_t):
-            if m is not None and m.device != self.device:
-                _refuse("out and out_t must be on the context's device")
         rm = None if row_mul is None else _vec(row_mul, "row_mul", rows, _torch().float32, self.device)
         cm = None if col_mul is None else _vec(col_mul, "col_mul", cols, x.dtype, self.device)
         _check(lib().jagg_quantize8(self._h, p, ld, rows, cols, dt, rm, cm, 1 if tile else 0,
-                                    None if out is None else out._c, None if out_t is None else out_t._c))
+                                    None if out is None else out._arg(self.device),
+                                    None if out_t is None else out_t._arg(self.device)))
         return out, out_t
 
     def matmul8(self, a: Mat8, b: Mat8, out, bias=None, beta: float = 0.0):
         """out = beta * out + a b^T + bias (out: [a.rows][b.rows], bf16 or fp32)."""
         dt = _dtype_of(out, "out")
         p, ld = _rows(out, "out", a.rows, b.rows, out.dtype, self.device)
-        if a.device != self.device or b.device != self.device:
-            _refuse("the operands must be on the context's device")
+        ac, bc = a._arg(self.device), b._arg(self.device)
         bp = None if bias is None else _vec(bias, "bias", b.rows, out.dtype, self.device)
         if a.rows > 16:
             nb = ctypes.c_size_t()
             _check(lib().jagg_matmul8_bytes(a.rows, b.rows, a.k, dt, ctypes.byref(nb)))
             if nb.value:
                 self._ensure_bytes(nb.value)
-        _check(lib().jagg_matmul8(self._h, a._c, b._c, bp, p, ld, dt, beta))
+        _check(lib().jagg_matmul8(self._h, ac, bc, bp, p, ld, dt, beta))
         return out
 
     def rmsnorm8(self, x, gain, y: Mat8, residual=None, h=None, rstd=None, eps: float = 1e-6):
@@ -579,10 +606,8 @@ class Context:
         p, ld = _rows(x, "x", rows, cols, x.dtype, dev)
         rp, rl = (None, 0) if residual is None else _rows(residual, "residual", rows, cols, x.dtype, dev)
         hp, hl = (None, 0) if h is None else _rows(h, "h", rows, cols, x.dtype, dev)
-        if y.device != dev:
-            _refuse("y must be on the context's device")
         _check(lib().jagg_rmsnorm8(self._h, p, ld, rp, rl, _vec(gain, "gain", cols, x.dtype, dev), rows, cols, dt, eps,
-                                   hp, hl, y._c, None if rstd is None else _vec(rstd, "rstd", rows, _torch().float32, dev)))
+                                   hp, hl, y._arg(dev), None if rstd is None else _vec(rstd, "rstd", rows, _torch().float32, dev)))
         return y
 
     def rmsnorm8_grad(self, dy, h, rstd, gain, dx, dgain, dh=None, beta: float = 0.0):
@@ -612,7 +637,7 @@ class Context:
             _refuse("the gradients must be on the context's device, ord 2 or inf")
         p = _vec(out, "out", 1, _torch().float64, self.device)
         self._ensure_bytes(_grad_bytes())
-        _check(lib().jagg_grad_norm(self._h, g._c, len(g.tensors), _NORMS[ord], p))
+        _check(lib().jagg_grad_norm(self._h, g._arg(), len(g.tensors), _NORMS[ord], p))
         return out
 
     def clip_grads(self, grads, max_norm: float, out, dst=None, ord=2):
@@ -633,7 +658,7 @@ class Context:
                 self._check_dst(g, d)
         p = _vec(out, "out", 2, _torch().float64, self.device)
         self._ensure_bytes(_grad_bytes())
-        _check(lib().jagg_grad_clip(self._h, g._c, None if d is None else d._c, len(g.tensors), _NORMS[ord],
+        _check(lib().jagg_grad_clip(self._h, g._arg(), None if d is None else d._arg(), len(g.tensors), _NORMS[ord],
                                     float(max_norm), p))
         return out
 
