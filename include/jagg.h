@@ -358,7 +358,9 @@ jagg_status jagg_linear_grad(jagg_ctx* ctx, int kind, const void* dY, const void
  * operands.  These calls enqueue on the context's stream, launch on its device
  * whichever is current, need no workspace unless they say so and may be
  * captured into a graph (graphs captured from one context share its workspace:
- * their replays must not overlap).  Device buffers must be aligned to their
+ * their replays must not overlap).  Sizes that would take 2^32 threads or more in one
+ * launch give EUNSUPPORTED (rmsnorm8: 2^26 rows up to 2048 columns, 2^24 up to 8192, 2^22
+ * above).  Device buffers must be aligned to their
  * elements and, where not said otherwise, must not overlap.  Row strides (ld..)
  * count elements. */
 typedef enum { JAGG_E4M3 = 0, JAGG_E5M2 = 1 } jagg_fmt8;

@@ -1377,8 +1377,6 @@ jagg_status jagg_quantize8(jagg_ctx* ctx, const void* x, size_t ldx, int rows, i
   if (out_t && (out_t->rows != cols || out_t->k != rows))
     return fail(JAGG_EINVAL, std::string(f) + "out_t must be cols x rows");
   if (out && out_t && out->fmt != out_t->fmt) return fail(JAGG_EINVAL, std::string(f) + "out and out_t differ in format");
-  if ((((size_t)rows + 127) / 128) * (((size_t)cols + 127) / 128) > 0x7fffffffu)
-    return fail(JAGG_EUNSUPPORTED, std::string(f) + "too many 128 x 128 tiles");
   jg::Quant8Args a{};
   a.x = x; a.ldx = ldx; a.rows = rows; a.cols = cols; a.dt = dtype;
   a.row_mul = row_mul; a.col_mul = col_mul; a.tile = tile;
@@ -1415,8 +1413,6 @@ jagg_status jagg_matmul8(jagg_ctx* ctx, const jagg_mat8* a, const jagg_mat8* b, 
   if (ldo < (size_t)b->rows) return fail(JAGG_EINVAL, std::string(f) + "ldo must be >= the right operand's rows");
   if (misaligned(out, jg::dsize(out_dtype)) || misaligned(bias, jg::dsize(out_dtype)))
     return fail(JAGG_EINVAL, std::string(f) + "a buffer is not aligned to its elements");
-  if ((((size_t)a->rows + 63) / 64) * (((size_t)b->rows + 63) / 64) > 0x7fffffffu)
-    return fail(JAGG_EUNSUPPORTED, std::string(f) + "too many tiles");
   jg::Matmul8Args g{};
   g.a = to_mat8(a); g.b = to_mat8(b);
   g.bias = bias;

@@ -1070,6 +1070,12 @@ static void launch_matmul8(const Matmul8Args& g, hipStream_t s) {
 }
 
 int matmul8(const Matmul8Args& g, hipStream_t s) {
+  const size_t M = g.a.rows, N = g.b.rows;
+  const size_t bm = g.kind == K8_128 ? 128 : g.kind == K8_256 ? 256 : 64, bn = g.kind == K8_32 ? 32 : bm;
+  const size_t wgs = g.kind == K8_FEW ? (N + 15) / 16 : (M + bm - 1) / bm * ((N + bn - 1) / bn);
+  const char* const many = "matmul8: too many rows";
+  if (int rc = too_many(wgs, g.kind == K8_FEW || (g.kind == K8_256 && g.out_dt == F32) ? 512 : 256, many)) return rc;
+  if (int rc = too_many(M > N ? M + 256 : N + 256, 2, many)) return rc;  // (row numbers of the last tile are ints)
   if (g.out_dt == BF16) {
     if (g.a.fmt == E5M2) launch_matmul8<E5M2, uint16_t>(g, s);
     else launch_matmul8<E4M3, uint16_t>(g, s);
@@ -1079,7 +1085,7 @@ int matmul8(const Matmul8Args& g, hipStream_t s) {
   }
   JG_CHECK_LAUNCH("matmul8");
   if (g.splits > 1) {
-    const size_t n = (size_t)g.a.rows * ((g.b.rows + 3) / 4);
+    const size_t n = M * ((N + 3) / 4);
     const dim3 grid((unsigned)((n + 255) / 256));
     if (g.out_dt == BF16) hipLaunchKernelGGL(matmul8_join_k<uint16_t>, grid, dim3(256), 0, s, g);
     else hipLaunchKernelGGL(matmul8_join_k<float>, grid, dim3(256), 0, s, g);

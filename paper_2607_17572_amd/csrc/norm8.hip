@@ -132,6 +132,8 @@ struct Norm8 {
 };
 
 int rmsnorm8(const Norm8Args& a, hipStream_t s) {
+  const unsigned nt = a.cols <= 2048 ? 64 : a.cols <= 8192 ? 256 : 1024;  // a row's threads (by_width)
+  if (int rc = too_many((size_t)a.rows + 3, nt, "rmsnorm8: too many rows")) return rc;
   if (a.dt == BF16) by_width<Norm8, uint16_t>(a, s);
   else by_width<Norm8, float>(a, s);
   JG_CHECK_LAUNCH("rmsnorm8");

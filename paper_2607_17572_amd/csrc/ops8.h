@@ -6,6 +6,13 @@
 
 namespace jg {
 
+// A launch has fewer than 2^32 threads along x.  Returns 4 (unsupported) for more.
+inline int too_many(size_t workgroups, unsigned threads, const char* what) {
+  if (workgroups * threads < (1ull << 32)) return 0;
+  set_error(std::string(what) + " for one launch (2^32 threads)");
+  return 4;
+}
+
 enum Fmt8 { E4M3 = 0, E5M2 = 1 };
 
 // 8-bit matrix of `rows` rows and k columns: bytes q[row * ld + col], zero from k to the

@@ -148,6 +148,8 @@ static void launch_quant8(const Quant8Args& a, hipStream_t s) {
 }
 
 int quant8(const Quant8Args& a, hipStream_t s) {
+  const size_t tiles = (((size_t)a.rows + 127) / 128) * (((size_t)a.cols + 127) / 128);
+  if (int rc = too_many(tiles, 256, "quantize8: too many 128 x 128 tiles")) return rc;
   if (a.dt == BF16) {
     if (a.fmt == E5M2) launch_quant8<uint16_t, E5M2>(a, s);
     else launch_quant8<uint16_t, E4M3>(a, s);
