@@ -424,8 +424,8 @@ jagg_status jagg_matmul8(jagg_ctx* ctx, const jagg_mat8* a, const jagg_mat8* b, 
  * rstd = 1 / sqrt(mean(h^2) + eps) over each row, y = (h rstd) gain in 8 bits
  * (E4M3, blocks of 128 elements of a row, as jagg_quantize8).
  *   x, residual, h: [rows][ld] of `dtype`; gain: cols of `dtype`; h may be NULL,
- *   and may be x or residual; y: rows x cols; rstd: rows floats or NULL (the
- *   backward needs it).  1 <= cols <= 32768 (EUNSUPPORTED above), eps >= 0. */
+ *   and may be x or residual (with its row stride); y: rows x cols; rstd: rows
+ *   floats or NULL (the backward needs it).  1 <= cols <= 32768 (EUNSUPPORTED above), eps >= 0. */
 jagg_status jagg_rmsnorm8(jagg_ctx* ctx, const void* x, size_t ldx, const void* residual, size_t ldr, const void* gain,
                           int rows, int cols, int dtype, float eps, void* h, size_t ldh, const jagg_mat8* y,
                           float* rstd);
@@ -435,9 +435,9 @@ jagg_status jagg_rmsnorm8(jagg_ctx* ctx, const void* x, size_t ldx, const void* 
  *   dx    = dh + rstd (a - h rstd^2 mean(a h))    (gradient of x and of residual)
  *   dgain = beta * dgain + sum over rows of dy h rstd
  * dy, h, dh, dx: [rows][ld] of `dtype`; dh (gradient of h from elsewhere) may be
- * NULL; dx may be dy or dh.  dgain: cols elements of dgain_dtype; beta 0 or 1.
- * Sums are fp32 in a fixed order.  Uses jagg_rmsnorm8_grad_bytes bytes of the
- * bound workspace. */
+ * NULL; dx may be dy or dh (with its row stride).  dgain: cols elements of
+ * dgain_dtype; beta 0 or 1.  Sums are fp32 in a fixed order.  Uses
+ * jagg_rmsnorm8_grad_bytes bytes of the bound workspace. */
 jagg_status jagg_rmsnorm8_grad_bytes(int rows, int cols, size_t* bytes);
 jagg_status jagg_rmsnorm8_grad(jagg_ctx* ctx, const void* dy, size_t lddy, const void* h, size_t ldh, const float* rstd,
                                const void* gain, const void* dh, size_t lddh, int rows, int cols, int dtype, void* dx,

@@ -1437,6 +1437,8 @@ jagg_status jagg_rmsnorm8(jagg_ctx* ctx, const void* x, size_t ldx, const void* 
   if (!(eps >= 0.f) || std::isinf(eps)) return fail(JAGG_EINVAL, std::string(f) + "eps must be >= 0 and finite");
   if (ldx < (size_t)cols || (residual && ldr < (size_t)cols) || (h && ldh < (size_t)cols))
     return fail(JAGG_EINVAL, std::string(f) + "row strides must be >= cols");
+  if (h && rows > 1 && ((h == x && ldh != ldx) || (h == residual && ldh != ldr)))
+    return fail(JAGG_EINVAL, std::string(f) + "h in place must have its input's row stride");
   const size_t es = jg::dsize(dtype);
   if (misaligned(x, es) || misaligned(residual, es) || misaligned(gain, es) || misaligned(h, es) || misaligned(rstd, 4))
     return fail(JAGG_EINVAL, std::string(f) + "a buffer is not aligned to its elements");
@@ -1469,6 +1471,8 @@ jagg_status jagg_rmsnorm8_grad(jagg_ctx* ctx, const void* dy, size_t lddy, const
   if (beta != 0.f && beta != 1.f) return fail(JAGG_EINVAL, std::string(f) + "beta must be 0 or 1");
   if (lddy < (size_t)cols || ldh < (size_t)cols || (dh && lddh < (size_t)cols) || lddx < (size_t)cols)
     return fail(JAGG_EINVAL, std::string(f) + "row strides must be >= cols");
+  if (rows > 1 && ((dx == dy && lddx != lddy) || (dx == dh && lddx != lddh)))
+    return fail(JAGG_EINVAL, std::string(f) + "dx in place must have its input's row stride");
   const size_t es = jg::dsize(dtype);
   if (misaligned(dy, es) || misaligned(h, es) || misaligned(gain, es) || misaligned(dh, es) || misaligned(dx, es) ||
       misaligned(rstd, 4) || misaligned(dgain, jg::dsize(dgain_dtype)))
