@@ -123,22 +123,9 @@ __global__ __launch_bounds__(256) void grad_norm_out_k(const double* part, int n
   if (threadIdx.x == 0) out[0] = norm;
 }
 
-// The factor in fp32, but for one below fp32's normal range: it would lose its digits,
-// or be 0 where the scaled values are not.
 template <typename T, typename D>
-__device__ __forceinline__ void scale_chunk(const T* p, D* d, unsigned n, double c64) {
+__device__ __forceinline__ void scale_chunk(const T* p, D* d, unsigned n, float c) {
   unsigned i = threadIdx.x * 8;
-  if (c64 < 0x1p-126) {
-    for (; i < n; i += 2048) {
-      float v[8];
-      load8(p, (int)i, (int)n, v);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (float)((double)v[e] * c64);
-      store8(d, (int)i, (int)n, v);
-    }
-    return;
-  }
-  const float c = (float)c64;
   if (n == CH) {
     float v[8][8];
 #pragma unroll
@@ -160,6 +147,20 @@ __device__ __forceinline__ void scale_chunk(const T* p, D* d, unsigned n, double
   }
 }
 
+// a value that all lanes share, in scalar registers
+__device__ __forceinline__ double scalar(double v) {
+  return __hiloint2double(__builtin_amdgcn_readfirstlane(__double2hiint(v)), __builtin_amdgcn_readfirstlane(__double2loint(v)));
+}
+
+// With a factor below fp32's normal range, where fp32 would lose its digits or make it 0.
+__device__ __noinline__ void scale_in_fp64(const void* src, void* dst, size_t at, unsigned n, int t, double c) {
+  for (size_t i = at + threadIdx.x; i < at + n; i += 256) {
+    const float v = (float)((double)(t & 1 ? ldf((const uint16_t*)src, i) : ldf((const float*)src, i)) * c);
+    if (t & 2) stf((uint16_t*)dst, i, v);
+    else stf((float*)dst, i, v);
+  }
+}
+
 template <bool MAX>
 __global__ __launch_bounds__(256) void grad_scale_k(GradSegs g, const double* part, int nparts, double max_norm,
                                                     double* out) {
@@ -167,8 +168,9 @@ __global__ __launch_bounds__(256) void grad_scale_k(GradSegs g, const double* pa
   const double norm = whole_norm<MAX>(part, nparts, sh);
   // false for NaN; an infinite norm keeps the gradients too
   const bool clip = norm > max_norm && norm <= 1.7976931348623157e308;
-  const double c = clip ? max_norm / norm : 1.0;
+  const double c = scalar(clip ? max_norm / norm : 1.0);
   if (out && blockIdx.x == 0 && threadIdx.x == 0) { out[0] = norm; out[1] = c; }
+  const float cf = (float)c;
   const Pieces pieces(g);
   for (unsigned k = blockIdx.x; k < g.chunks; k += gridDim.x) {
     const int s = pieces.of(k);
@@ -176,10 +178,11 @@ __global__ __launch_bounds__(256) void grad_scale_k(GradSegs g, const double* pa
     const size_t at = (size_t)(k - g.first[s]) * g.ch, left = g.n[s] - at;
     const unsigned n = left < g.ch ? (unsigned)left : g.ch;
     const int t = g.dt[s];
-    if (t == 3) scale_chunk((const uint16_t*)g.src[s] + at, (uint16_t*)g.dst[s] + at, n, c);
-    else if (t == 1) scale_chunk((const uint16_t*)g.src[s] + at, (float*)g.dst[s] + at, n, c);
-    else if (t == 2) scale_chunk((const float*)g.src[s] + at, (uint16_t*)g.dst[s] + at, n, c);
-    else scale_chunk((const float*)g.src[s] + at, (float*)g.dst[s] + at, n, c);
+    if (c < 0x1p-126) scale_in_fp64(g.src[s], g.dst[s], at, n, t, c);
+    else if (t == 3) scale_chunk((const uint16_t*)g.src[s] + at, (uint16_t*)g.dst[s] + at, n, cf);
+    else if (t == 1) scale_chunk((const uint16_t*)g.src[s] + at, (float*)g.dst[s] + at, n, cf);
+    else if (t == 2) scale_chunk((const float*)g.src[s] + at, (uint16_t*)g.dst[s] + at, n, cf);
+    else scale_chunk((const float*)g.src[s] + at, (float*)g.dst[s] + at, n, cf);
   }
 }
 
