@@ -912,7 +912,7 @@ __global__ __launch_bounds__(512) void matmul8_few_k(Matmul8Args g) {
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int u = 0; u < UU; ++u) {
-      large |= large_scales((wa[u] >> sh) & 255u) | large_scales((wb[u] >> sh) & 255u);
+      large |= large_scales(wa[u]) | large_scales(wb[u]);
 #pragma unroll
       for (int w = 0; w < 8; w += 2)
         acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<E4M3>(fb[u][w], fb[u][w + 1], scale_of((wb[u] >> sh) & 255u)),
