@@ -879,9 +879,10 @@ __global__ __launch_bounds__(256) void matmul8_quad_k(Matmul8Args g) {
 // waves every eighth block of 128 (neighbouring blocks of a row are read together),
 // operands straight to registers with four blocks in flight a wave.  The waves' sums
 // are added through LDS in wave order.  A lane takes chunks q and q + 4 of a row's block
-// (q = lane / 16), the same on both sides.  One row, 16384 x 4096 (68 MB): 13.5 us,
-// 5.0 TB/s; 4096 x 12288: 10.9 us (32 rows of B a workgroup: 14.5 and 15.5; two blocks
-// in flight: 16.3 and 10.0).
+// (q = lane / 16), the same on both sides.  One row, 16384 x 4096 (68 MB from memory): 15.8
+// us, 4.3 TB/s; 4096 x 12288 (50 MB): 13.2.  With four weights in turn, which the 256 MB
+// cache holds in part: 13.5 and 10.9, where 32 rows of B a workgroup took 14.5 and 15.5, two
+// blocks in flight 16.3 and 10.0 (these six with the 8-bit instruction).
 template <int FA, typename T>
 __global__ __launch_bounds__(512) void matmul8_few_k(Matmul8Args g) {
   constexpr int KW = 8, U = 4;
