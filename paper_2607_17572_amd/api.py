@@ -344,7 +344,8 @@ _NORMS = {2: 0, 2.0: 0, float("inf"): 1}
 
 
 class Context:
-    """One model configuration bound to a HIP stream, with a workspace tensor."""
+    """One model configuration bound to a HIP stream, with a workspace tensor.  Every call
+    runs on that stream, whichever is current."""
 
     def __init__(self, cfg: Config, stream=None):
         torch = _torch()
@@ -583,7 +584,8 @@ class Context:
         return out, out_t
 
     def matmul8(self, a: Mat8, b: Mat8, out, bias=None, beta: float = 0.0):
-        """out = beta * out + a b^T + bias (out: [a.rows][b.rows], bf16 or fp32)."""
+        """out = beta * out + a b^T + bias (out: [a.rows][b.rows], bf16 or fp32).  The sums
+        are fp32, but for large bf16 results: there the 8-bit matrix instructions'."""
         dt = _dtype_of(out, "out")
         p, ld = _rows(out, "out", a.rows, b.rows, out.dtype, self.device)
         ac, bc = a._arg(self.device), b._arg(self.device)
